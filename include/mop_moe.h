@@ -250,6 +250,39 @@ mop_status mop_moe_route_bwd(mop_ctx* ctx, const float* logits, const float* bia
                              const int32_t* perm_row, const float* W_r, float* dW_r, float* dbias_opt, void* dX,
                              void* stream);
 
+/* Load-balance loss of the router with the per-expert counts, and its gradients (the MoE block of Section 2.1 is trained with one;
+ * the paper names none, so the formulas stand here).  The T tokens are a packed batch: sequence s holds the tokens
+ * seq_offsets[s] <= t < seq_offsets[s+1], T_s of them; tokens in front of the first and behind the last sequence are padding and
+ * are not read.  With z the logits (plus the bias for MOP_BIAS_PRE_LOGIT; a post-score bias only steers the selection),
+ *   p[t,e]      = softmax_e(z[t,:])   |   sigmoid(z[t,e]) / sum_e' sigmoid(z[t,e'])         (score_fn)
+ *   counts[s,e] = number of picks topk_idx[t,j] = e of the sequence's tokens;   prob[s,e] = 1 / T_s sum_t p[t,e]
+ *   loss[s]     = E / (k T_s) sum_e counts[s,e] prob[s,e]                 (1 when every expert gets the same share)
+ * A sequence without tokens has zero counts, prob and loss.  A logit of -inf masks an expert; a token whose experts are all masked
+ * adds nothing to prob.  Picks outside [0,E) are not counted.
+ * logits [T,E] f32 (from mop_moe_route); topk_idx [T,k]; seq_offsets [n_seq+1] i32, non-decreasing within [0,T], or NULL with
+ * n_seq = 1: one sequence of all T tokens; counts [n_seq,E] i32, prob [n_seq,E] f32, loss [n_seq] f32 out; workspace:
+ * mop_moe_balance_workspace_bytes(shape, n_seq, 0) bytes of device memory, 256-byte aligned, owned by the caller. */
+size_t mop_moe_balance_workspace_bytes(const mop_moe_shape* shape, int32_t n_seq, int32_t with_backward);
+mop_status mop_moe_balance_loss_fwd(mop_ctx* ctx, int32_t n_seq, const float* logits, const float* bias, const int32_t* topk_idx,
+                                    const int32_t* seq_offsets, int32_t* counts, float* prob, float* loss, void* workspace,
+                                    void* stream);
+
+/* Gradients of sum_s dloss[s] loss[s], the counts held fixed:  with c[e] = dloss[s] E / (k T_s^2) counts[s,e] and
+ * m = sum_e p[t,e] c[e],
+ *   softmax:  dz[t,e] = p[t,e] (c[e] - m)          sigmoid:  dz[t,e] = p[t,e] (1 - sigmoid(z[t,e])) (c[e] - m)
+ *   dW_r = x^T dz,   dX = dz W_r^T,   dbias = column sums of dz (MOP_BIAS_PRE_LOGIT; zero in the other modes)
+ * and dz = 0 for padding tokens.  accumulate = 0 overwrites dW_r, dbias and dX (rows of padding tokens get zeros); 1 adds to them
+ * (rows of padding tokens stay as they are), as is wanted behind mop_moe_route_bwd, which writes dW_r and adds to the same dX.
+ * dlogits is always overwritten.  Any of the four outputs may be NULL, not all.  dW_r has fp32 accuracy; dX is rounded to bf16 once.
+ * counts [n_seq,E] i32 from the forward (or their totals over several devices: dz is linear in them); dloss [n_seq] f32;
+ * x [T,d] bf16 (needed for dW_r; rows of padding tokens are not read into it, whatever they hold); W_r [d,E] f32 (needed for dX);
+ * dlogits_opt [T,E] f32, dW_r_opt [d,E] f32, dbias_opt [E] f32, dX_opt [T,d] bf16 out; workspace:
+ * mop_moe_balance_workspace_bytes(shape, n_seq, 1) bytes.  Needs no context with backward buffers. */
+mop_status mop_moe_balance_loss_bwd(mop_ctx* ctx, int32_t n_seq, const float* logits, const float* bias, const int32_t* seq_offsets,
+                                    const int32_t* counts, const float* dloss, const void* x, const float* W_r, int32_t accumulate,
+                                    float* dlogits_opt, float* dW_r_opt, float* dbias_opt, void* dX_opt, void* workspace,
+                                    void* stream);
+
 /* Whole forward with HOST buffers (pageable or pinned): copies x in, runs route, permute,
  * expert_ffn_fwd and combine on `stream`, copies Y, topk_idx and topk_gate back, and
  * synchronises.  Weights stay on the device (they are parameters, not step inputs).

@@ -321,3 +321,54 @@ def vocab_loss_bwd(x_bits, W_bits, targets, dloss, declared=False):
         dY = bf16_bits_to_f64(f32_to_bf16_bits(dY.astype(np.float32)))
     return dY @ W.T, X.T @ dY
 
+
+
+# ----------------------------------------------------------------------------- load-balance loss
+def _balance_scores(logits, bias, score_fn, bias_mode):
+    z = np.asarray(logits, np.float64)
+    if bias_mode == BIAS_PRE_LOGIT:
+        z = z + np.asarray(bias, np.float64)[None, :]
+    if score_fn == SCORE_SOFTMAX:
+        m = z.max(1, keepdims=True)
+        s = np.exp(z - np.where(np.isfinite(m), m, 0.0))
+    else:
+        s = np.where(z >= 0, 1.0 / (1.0 + np.exp(-np.abs(z))), np.exp(-np.abs(z)) / (1.0 + np.exp(-np.abs(z))))
+    S = s.sum(1, keepdims=True)
+    return s, np.divide(s, S, out=np.zeros_like(s), where=S != 0), S
+
+
+def balance_loss(logits, bias, k, score_fn, bias_mode, idx, seq_offsets):
+    """Load-balance loss per sequence (plain numpy, fp64): with p the normalised scores of the tokens of a sequence,
+        counts[e] = picks of expert e,  P[e] = mean of p[:, e],  loss = E / (k T_s) sum_e counts[e] P[e].
+    seq_offsets [S+1].  Returns (counts [S,E] int, prob [S,E], loss [S])."""
+    off = np.asarray(seq_offsets, np.int64)
+    E = np.asarray(logits).shape[1]
+    S = off.size - 1
+    counts, prob, loss = np.zeros((S, E), np.int64), np.zeros((S, E)), np.zeros(S)
+    for s in range(S):
+        a, b = int(off[s]), int(off[s + 1])
+        if a == b:
+            continue
+        _, p, _ = _balance_scores(logits[a:b], bias, score_fn, bias_mode)
+        picks = np.asarray(idx[a:b], np.int64).reshape(-1)
+        counts[s] = np.bincount(picks[(picks >= 0) & (picks < E)], minlength=E)
+        prob[s] = p.sum(0) / (b - a)
+        loss[s] = E / (k * (b - a)) * (counts[s] * prob[s]).sum()
+    return counts, prob, loss
+
+
+def balance_loss_bwd(logits, bias, k, score_fn, bias_mode, counts, seq_offsets, dloss):
+    """dz [T,E] of sum_s dloss[s] loss[s] with the counts held fixed (plain numpy, fp64), written out from the quotient
+    p = s / sum s and the score's own derivative; zero for tokens outside the sequences."""
+    off = np.asarray(seq_offsets, np.int64)
+    dz = np.zeros(np.asarray(logits).shape)
+    E = dz.shape[1]
+    for s in range(off.size - 1):
+        a, b = int(off[s]), int(off[s + 1])
+        if a == b:
+            continue
+        sc, p, S = _balance_scores(logits[a:b], bias, score_fn, bias_mode)
+        dp = float(dloss[s]) * E / (k * (b - a) ** 2) * np.asarray(counts[s], np.float64)[None, :]
+        ds = np.divide(dp - (dp * p).sum(1, keepdims=True), S, out=np.zeros_like(p), where=S != 0)
+        dz[a:b] = ds * (sc if score_fn == SCORE_SOFTMAX else sc * (1.0 - sc))
+    return dz

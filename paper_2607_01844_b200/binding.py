@@ -70,6 +70,10 @@ def lib() -> ctypes.CDLL:
         L.mop_moe_train_step_host_async.argtypes = [_P] * 15
         L.mop_host_drain.argtypes = [_P] * 2
         L.mop_moe_route_bwd.argtypes = [_P] * 14
+        L.mop_moe_balance_workspace_bytes.argtypes = [ctypes.POINTER(MopShape), ctypes.c_int32, ctypes.c_int32]
+        L.mop_moe_balance_workspace_bytes.restype = ctypes.c_size_t
+        L.mop_moe_balance_loss_fwd.argtypes = [_P, ctypes.c_int32] + [_P] * 9
+        L.mop_moe_balance_loss_bwd.argtypes = [_P, ctypes.c_int32] + [_P] * 7 + [ctypes.c_int32] + [_P] * 6
         L.mop_moe_chunked_workspace_bytes.argtypes = [ctypes.POINTER(MopShape), ctypes.c_int32, ctypes.c_int32]
         L.mop_moe_chunked_workspace_bytes.restype = ctypes.c_size_t
         L.mop_moe_layer_fwd_chunked.argtypes = [_P, ctypes.c_int32] + [_P] * 15
@@ -230,6 +234,26 @@ def mop_moe_route_bwd(ctx, logits, bias, topk_idx, topk_gate, dgate, Xp, offsets
            lib().mop_moe_route_bwd(ctx.handle, _ptr(logits), _ptr(bias), _ptr(topk_idx), _ptr(topk_gate), _ptr(dgate),
                                    _ptr(Xp), _ptr(offsets), _ptr(perm_row), _ptr(W_r), _ptr(dW_r), _ptr(dbias),
                                    _ptr(dX), _stream(stream)))
+
+
+def mop_moe_balance_workspace_bytes(ctx, n_seq, with_backward=False):
+    return lib().mop_moe_balance_workspace_bytes(ctypes.byref(ctx.shape), n_seq, int(with_backward))
+
+
+def mop_moe_balance_loss_fwd(ctx, logits, bias, topk_idx, seq_offsets, counts, prob, loss, workspace, stream=None):
+    """Per sequence of a packed batch: expert counts, mean scores and the load-balance loss."""
+    _check("mop_moe_balance_loss_fwd",
+           lib().mop_moe_balance_loss_fwd(ctx.handle, loss.shape[0], _ptr(logits), _ptr(bias), _ptr(topk_idx), _ptr(seq_offsets),
+                                          _ptr(counts), _ptr(prob), _ptr(loss), _ptr(workspace), _stream(stream)))
+
+
+def mop_moe_balance_loss_bwd(ctx, logits, bias, seq_offsets, counts, dloss, x, W_r, dlogits, dW_r, dbias, dX, accumulate, workspace,
+                             stream=None):
+    """Gradients of sum_s dloss[s] loss[s]; outputs that are None are not computed."""
+    _check("mop_moe_balance_loss_bwd",
+           lib().mop_moe_balance_loss_bwd(ctx.handle, dloss.shape[0], _ptr(logits), _ptr(bias), _ptr(seq_offsets), _ptr(counts),
+                                          _ptr(dloss), _ptr(x), _ptr(W_r), int(accumulate), _ptr(dlogits), _ptr(dW_r), _ptr(dbias),
+                                          _ptr(dX), _ptr(workspace), _stream(stream)))
 
 
 def mop_moe_chunked_workspace_bytes(ctx, n_chunks, with_backward=False):

@@ -14,6 +14,7 @@
 #include "gemm_host.cuh"
 #include "gemm_rs.cuh"
 #include "route_permute.cuh"
+#include "balance.cuh"
 
 using namespace mop;
 
@@ -1149,6 +1150,129 @@ mop_status mop_moe_route_bwd(mop_ctx* c, const float* logits, const float* bias,
            pdl_launch(route_bwd_dwr_dx_kernel, dwr_blocks + dx_blocks, 32 * dwr_w, dwr_w * 1024, st, static_cast<const bf16*>(Xp),
                       c->dz_row, offsets, dW_r, db, s.d, s.E, c->wrT, topk_idx, c->dz_sel, static_cast<bf16*>(dX), s.T, s.k));
     return after_launch(c);
+}
+
+// ---------------------------------------------------------------------------------------------
+// Load-balance loss of the router and its gradients (the caller owns the workspace)
+// ---------------------------------------------------------------------------------------------
+namespace {
+struct BalanceLayout { size_t part_p, part_c, dz, dbias, total; };
+BalanceLayout balance_layout(const mop_moe_shape& s, bool backward) {
+    BalanceLayout L{};
+    size_t o = 0;
+    auto take = [&](size_t b) { size_t r = o; o += align_up(b); return r; };
+    const size_t blocks = bal_blocks(s.T), E = s.E;
+    if (!backward) {
+        L.part_p = take(2 * blocks * E * 4);
+        L.part_c = take(2 * blocks * E * 4);
+    } else {
+        L.dz = take((size_t)s.T * E * 4);
+        L.dbias = take(blocks * E * 4);
+    }
+    L.total = o;
+    return L;
+}
+bool balance_n_seq_ok(const mop_moe_shape& s, int32_t n_seq) { return n_seq >= 1 && (long long)n_seq * s.E < (1ll << 31); }
+}  // namespace
+
+size_t mop_moe_balance_workspace_bytes(const mop_moe_shape* shape, int32_t n_seq, int32_t with_backward) {
+    if (check_shape(shape) != MOP_OK || !balance_n_seq_ok(*shape, n_seq)) return 0;
+    return balance_layout(*shape, with_backward != 0).total;
+}
+
+mop_status mop_moe_balance_loss_fwd(mop_ctx* c, int32_t n_seq, const float* logits, const float* bias, const int32_t* topk_idx,
+                                    const int32_t* seq_offsets, int32_t* counts, float* prob, float* loss, void* workspace,
+                                    void* stream) {
+    if (!c) return MOP_ERR_INVALID_ARG;
+    if (n_seq < 1 || (!seq_offsets && n_seq != 1)) return MOP_ERR_INVALID_ARG;
+    if (!balance_n_seq_ok(c->s, n_seq)) return MOP_ERR_SHAPE;
+    REQ_PTR_T(logits); REQ_PTR_T(topk_idx); REQ_PTR(counts); REQ_PTR(prob); REQ_PTR(loss); REQ_PTR_T(workspace);
+    if ((c->s.bias_mode != MOP_BIAS_NONE) != (bias != nullptr)) return MOP_ERR_INVALID_ARG;
+    if (!aligned16(bias) || !aligned16(seq_offsets) || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return MOP_ERR_ALIGN;
+    const mop_moe_shape& s = c->s;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return MOP_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (s.T == 0) {
+        CUDA_OK(cudaMemsetAsync(counts, 0, (size_t)n_seq * s.E * 4, st));
+        CUDA_OK(cudaMemsetAsync(prob, 0, (size_t)n_seq * s.E * 4, st));
+        CUDA_OK(cudaMemsetAsync(loss, 0, (size_t)n_seq * 4, st));
+        return MOP_OK;
+    }
+    const BalanceLayout L = balance_layout(s, false);
+    char* w = static_cast<char*>(workspace);
+    BalFwdArgs a{};
+    a.logits = logits; a.bias = s.bias_mode == MOP_BIAS_PRE_LOGIT ? bias : nullptr; a.idx = topk_idx;
+    a.q = {seq_offsets, n_seq, s.T}; a.s = bal_shape(s); a.chunk = bal_chunk(s.T);
+    a.counts = counts; a.prob = prob; a.loss = loss;
+    a.part_p = reinterpret_cast<float*>(w + L.part_p); a.part_c = reinterpret_cast<int32_t*>(w + L.part_c);
+    const int warps = bal_warps(s.E);
+#define GO(NV) pdl_launch(balance_fwd_kernel<NV>, bal_blocks(s.T), 32 * warps, bal_smem_bytes(s.E, warps), st, a)
+    LAUNCH(c, "balance_fwd", st, BAL_BY_WIDTH(s.E, GO));
+#undef GO
+    mop_status r = after_launch(c);
+    if (r != MOP_OK) return r;
+    LAUNCH(c, "balance_finish", st, pdl_launch(balance_finish_kernel, min(n_seq, 1184), 1024, 0, st, a));
+    return after_launch(c);
+}
+
+mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logits, const float* bias, const int32_t* seq_offsets,
+                                    const int32_t* counts, const float* dloss, const void* x, const float* W_r, int32_t accumulate,
+                                    float* dlogits_opt, float* dW_r_opt, float* dbias_opt, void* dX_opt, void* workspace,
+                                    void* stream) {
+    if (!c) return MOP_ERR_INVALID_ARG;
+    if (n_seq < 1 || (!seq_offsets && n_seq != 1)) return MOP_ERR_INVALID_ARG;
+    if (accumulate != 0 && accumulate != 1) return MOP_ERR_INVALID_ARG;
+    if (!balance_n_seq_ok(c->s, n_seq)) return MOP_ERR_SHAPE;
+    if (!dlogits_opt && !dW_r_opt && !dX_opt && !dbias_opt) return MOP_ERR_INVALID_ARG;
+    REQ_PTR_T(logits); REQ_PTR(counts); REQ_PTR(dloss); REQ_PTR_T(workspace);
+    if (dW_r_opt) REQ_PTR_T(x);
+    if (dX_opt) REQ_PTR(W_r);
+    if ((c->s.bias_mode != MOP_BIAS_NONE) != (bias != nullptr)) return MOP_ERR_INVALID_ARG;
+    if (!aligned16(bias) || !aligned16(seq_offsets) || !aligned16(dlogits_opt) || !aligned16(dW_r_opt) || !aligned16(dbias_opt) ||
+        !aligned16(dX_opt) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+        return MOP_ERR_ALIGN;
+    const mop_moe_shape& s = c->s;
+    DeviceGuard guard(c->device);
+    if (!guard.ok) return MOP_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool pre = s.bias_mode == MOP_BIAS_PRE_LOGIT;
+    if (dbias_opt && !accumulate && (!pre || s.T == 0)) CUDA_OK(cudaMemsetAsync(dbias_opt, 0, (size_t)s.E * 4, st));
+    if (s.T == 0) {
+        if (dW_r_opt && !accumulate) CUDA_OK(cudaMemsetAsync(dW_r_opt, 0, (size_t)s.d * s.E * 4, st));
+        return MOP_OK;
+    }
+    const BalanceLayout L = balance_layout(s, true);
+    char* w = static_cast<char*>(workspace);
+    BalBwdArgs a{};
+    a.logits = logits; a.bias = pre ? bias : nullptr; a.counts = counts; a.dloss = dloss;
+    a.q = {seq_offsets, n_seq, s.T}; a.s = bal_shape(s); a.chunk = bal_chunk(s.T);
+    a.dz = dlogits_opt ? dlogits_opt : reinterpret_cast<float*>(w + L.dz);
+    a.dbias_part = pre && dbias_opt ? reinterpret_cast<float*>(w + L.dbias) : nullptr;
+    const int warps = bal_warps(s.E), blocks = bal_blocks(s.T);
+#define GO(NV) pdl_launch(balance_dz_kernel<NV>, blocks, 32 * warps, bal_smem_bytes(s.E, warps), st, a)
+    LAUNCH(c, "balance_dz", st, BAL_BY_WIDTH(s.E, GO));
+#undef GO
+    mop_status r = after_launch(c);
+    if (r != MOP_OK) return r;
+    if (a.dbias_part) {
+        LAUNCH(c, "balance_dbias", st,
+               pdl_launch(balance_dbias_kernel, ceil_div(s.E, 256), 256, 0, st, a.dbias_part, dbias_opt, blocks, s.E, accumulate));
+        if ((r = after_launch(c)) != MOP_OK) return r;
+    }
+    if (dW_r_opt) {
+        LAUNCH(c, "balance_dw", st,
+               pdl_launch(balance_dw_kernel, dim3(ceil_div(s.d, 64), ceil_div(s.E, 64)), 256, 0, st, static_cast<const bf16*>(x), a.dz,
+                          a.q, dW_r_opt, s.d, s.E, accumulate));
+        if ((r = after_launch(c)) != MOP_OK) return r;
+    }
+    if (dX_opt) {
+        LAUNCH(c, "balance_dx", st,
+               pdl_launch(balance_dx_kernel, dim3(ceil_div(s.d, 64), ceil_div(s.T, 64)), 256, 0, st, a.dz, W_r, a.q,
+                          static_cast<bf16*>(dX_opt), s.T, s.d, s.E, accumulate));
+        r = after_launch(c);
+    }
+    return r;
 }
 
 namespace {
