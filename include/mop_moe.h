@@ -371,6 +371,36 @@ mop_status mop_vocab_loss_bwd(int device, int32_t N, int32_t H, int32_t V, const
                               const int32_t* targets, const float* lse, const float* dloss, void* dX,
                               float* dW_voc, void* workspace, void* stream);
 
+/* Distillation through the same projection from a teacher's top logits: per token the teacher gives K of its logits t[n,k] with their
+ * places teacher_idx[n,k] in the vocabulary (entries outside [0,V) are ignored, so a list may be shorter than K; a token without
+ * entries has no loss and no gradient).  With Y = X W_voc, s = Y / temperature, lse[n] = log sum_v exp s[n,v] and the teacher's probabilities
+ *   q[n,k] = exp(t[n,k] / temperature) / sum_j exp(t[n,j] / temperature),   or, where the teacher's own log-sum-exp over its whole
+ *   vocabulary of t / temperature is given,  q[n,k] = exp(t[n,k] / temperature - teacher_lse[n])
+ * the loss is the Kullback-Leibler divergence over the teacher's entries
+ *   loss[n] = sum_k q[n,k] (log q[n,k] - s[n, teacher_idx[n,k]] + lse[n])
+ * (the usual factor temperature^2 is the caller's, by dloss).  The N x V logits are never stored: tile by tile a running maximum and sum,
+ * and the logits at the teacher's places.  A place that is named more than once counts each time.
+ * X [N,H] bf16; W_voc [H,V] bf16; teacher_idx [N,K] i32; teacher_logits [N,K] f32; teacher_lse_opt [N] f32 or NULL; temperature > 0;
+ * loss [N] f32, student [N,K] f32 (Y at the teacher's places, 0 for ignored entries), lse [N] f32 out.  H and V must be multiples
+ * of 8, 1 <= K <= 256.  workspace: mop_vocab_distill_workspace_bytes bytes of device memory, 256-byte aligned, owned by the caller;
+ * mop_vocab_poll reads it as for the calls above. */
+size_t mop_vocab_distill_workspace_bytes(int32_t N, int32_t H, int32_t V, int32_t K);
+mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, int32_t K, const void* X, const void* W_voc,
+                                 const int32_t* teacher_idx, const float* teacher_logits, const float* teacher_lse_opt,
+                                 float temperature, float* loss, float* student, float* lse, void* workspace, void* stream);
+
+/* Its gradients, with an upstream weight dloss[n] per token and Q[n] = sum_k q[n,k]:
+ *   dY[n,v] = dloss[n] / temperature (Q[n] exp(s[n,v] - lse[n]) - sum of the q[n,k] with teacher_idx[n,k] = v),
+ *   dX = dY W_voc^T,   dW_voc = X^T dY
+ * in blocks of 8192 vocabulary columns, as mop_vocab_loss_bwd.  student and lse are the forward's.  dX [N,H] bf16 out, dW_voc [H,V]
+ * bf16 out (both overwritten; dY is rounded to bf16 before its products, so fp32 would hold no more).
+ * workspace: mop_vocab_distill_bwd_workspace_bytes bytes. */
+size_t mop_vocab_distill_bwd_workspace_bytes(int32_t N, int32_t H, int32_t V, int32_t K);
+mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, int32_t K, const void* X, const void* W_voc,
+                                 const int32_t* teacher_idx, const float* teacher_logits, const float* teacher_lse_opt,
+                                 float temperature, const float* student, const float* lse, const float* dloss, void* dX,
+                                 void* dW_voc, void* workspace, void* stream);
+
 /* The same permutation as mop_moe_permute for callers that may not allocate device memory (the
  * paper has no counterpart; this is a property of the library, not of the method).  A process
  * that gave all of HBM to its own arena, or a loop that cannot take the device-wide

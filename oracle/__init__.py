@@ -372,3 +372,44 @@ def balance_loss_bwd(logits, bias, k, score_fn, bias_mode, counts, seq_offsets, 
         ds = np.divide(dp - (dp * p).sum(1, keepdims=True), S, out=np.zeros_like(p), where=S != 0)
         dz[a:b] = ds * (sc if score_fn == SCORE_SOFTMAX else sc * (1.0 - sc))
     return dz
+
+
+# ----------------------------------------------------------------------------- distillation through the projection
+def _teacher(ids, t, tau, V, teacher_lse):
+    """Teacher's probabilities [N,K] (0 for entries outside the vocabulary) and their logarithms."""
+    ids = np.asarray(ids, np.int64)
+    valid = (ids >= 0) & (ids < V)
+    s = np.where(valid, np.asarray(t, np.float64) / tau, -np.inf)
+    if teacher_lse is None:
+        m = s.max(1, keepdims=True)
+        m = np.where(np.isfinite(m), m, 0.0)
+        S = np.exp(s - m).sum(1, keepdims=True)
+        logq = s - m - np.log(np.where(S > 0, S, 1.0))
+    else:
+        logq = s - np.asarray(teacher_lse, np.float64)[:, None]
+    return valid, np.exp(logq), logq
+
+
+def vocab_distill(x_bits, W_bits, ids, t, tau, teacher_lse=None):
+    """Divergence of the student's distribution from the teacher's entries (plain numpy, fp64): with s = X W_voc / tau,
+        loss[n] = sum_k q[n,k] (log q[n,k] - log softmax(s[n])[ids[n,k]]).
+    Returns (loss [N], student [N,K], lse [N])."""
+    Y = bf16_bits_to_f64(x_bits) @ bf16_bits_to_f64(W_bits)
+    valid, q, logq = _teacher(ids, t, tau, Y.shape[1], teacher_lse)
+    m = (Y / tau).max(1, keepdims=True)
+    lse = (m + np.log(np.exp(Y / tau - m).sum(1, keepdims=True)))[:, 0]
+    student = np.where(valid, np.take_along_axis(Y, np.where(valid, ids, 0).astype(np.int64), 1), 0.0)
+    terms = q * (np.where(q > 0, logq, 0.0) - (student / tau - lse[:, None]))
+    return np.where(q > 0, terms, 0.0).sum(1), student, lse
+
+
+def vocab_distill_dlogits(x_bits, W_bits, ids, t, tau, dloss, teacher_lse=None):
+    """Gradient [N,V] of sum_n dloss[n] loss[n] with respect to the logits X W_voc: every entry pulls the softmax towards its place."""
+    Y = bf16_bits_to_f64(x_bits) @ bf16_bits_to_f64(W_bits)
+    valid, q, _ = _teacher(ids, t, tau, Y.shape[1], teacher_lse)
+    p = np.exp(Y / tau - (Y / tau).max(1, keepdims=True))
+    p /= p.sum(1, keepdims=True)
+    dY = q.sum(1, keepdims=True) * p
+    for n, k in zip(*np.nonzero(valid)):
+        dY[n, ids[n, k]] -= q[n, k]
+    return dY * (np.asarray(dloss, np.float64) / tau)[:, None]

@@ -88,6 +88,12 @@ def lib() -> ctypes.CDLL:
         L.mop_vocab_bwd_workspace_bytes.argtypes = [ctypes.c_int32] * 3
         L.mop_vocab_bwd_workspace_bytes.restype = ctypes.c_size_t
         L.mop_vocab_loss_bwd.argtypes = [ctypes.c_int] + [ctypes.c_int32] * 3 + [_P] * 9
+        L.mop_vocab_distill_workspace_bytes.argtypes = [ctypes.c_int32] * 4
+        L.mop_vocab_distill_workspace_bytes.restype = ctypes.c_size_t
+        L.mop_vocab_distill_fwd.argtypes = [ctypes.c_int] + [ctypes.c_int32] * 4 + [_P] * 5 + [ctypes.c_float] + [_P] * 5
+        L.mop_vocab_distill_bwd_workspace_bytes.argtypes = [ctypes.c_int32] * 4
+        L.mop_vocab_distill_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.mop_vocab_distill_bwd.argtypes = [ctypes.c_int] + [ctypes.c_int32] * 4 + [_P] * 5 + [ctypes.c_float] + [_P] * 7
         L.mop_profile_enable.argtypes = [_P, ctypes.c_int]
         L.mop_profile_read.argtypes = [_P, _P, ctypes.c_int32, ctypes.POINTER(ctypes.c_char_p),
                                        ctypes.POINTER(ctypes.c_float), ctypes.POINTER(ctypes.c_int32)]
@@ -364,6 +370,40 @@ def mop_vocab_loss_bwd(device, X, W_voc, targets, lse, dloss, dX, dW_voc, worksp
     _check("mop_vocab_loss_bwd",
            lib().mop_vocab_loss_bwd(device, N, H, V, _ptr(X), _ptr(W_voc), _ptr(targets), _ptr(lse), _ptr(dloss),
                                     _ptr(dX), _ptr(dW_voc), _ptr(workspace), _stream(stream)))
+    return workspace
+
+
+def mop_vocab_distill_workspace_bytes(N, H, V, K):
+    return lib().mop_vocab_distill_workspace_bytes(N, H, V, K)
+
+
+def mop_vocab_distill_fwd(device, X, W_voc, teacher_idx, teacher_logits, temperature, loss, student, lse, teacher_lse=None,
+                          workspace=None, stream=None):
+    """loss[n] = KL divergence of the student from the teacher over the teacher's entries; student = logits at those entries."""
+    (N, H), V, K = X.shape, W_voc.shape[1], teacher_idx.shape[1]
+    if workspace is None:
+        workspace = torch.empty(max(256, mop_vocab_distill_workspace_bytes(N, H, V, K)), dtype=torch.uint8, device=X.device)
+    _check("mop_vocab_distill_fwd",
+           lib().mop_vocab_distill_fwd(device, N, H, V, K, _ptr(X), _ptr(W_voc), _ptr(teacher_idx), _ptr(teacher_logits),
+                                       _ptr(teacher_lse), temperature, _ptr(loss), _ptr(student), _ptr(lse), _ptr(workspace),
+                                       _stream(stream)))
+    return workspace
+
+
+def mop_vocab_distill_bwd_workspace_bytes(N, H, V, K):
+    return lib().mop_vocab_distill_bwd_workspace_bytes(N, H, V, K)
+
+
+def mop_vocab_distill_bwd(device, X, W_voc, teacher_idx, teacher_logits, temperature, student, lse, dloss, dX, dW_voc,
+                          teacher_lse=None, workspace=None, stream=None):
+    """dX, dW_voc of sum_n dloss[n] loss[n]; student and lse are the forward's."""
+    (N, H), V, K = X.shape, W_voc.shape[1], teacher_idx.shape[1]
+    if workspace is None:
+        workspace = torch.empty(max(256, mop_vocab_distill_bwd_workspace_bytes(N, H, V, K)), dtype=torch.uint8, device=X.device)
+    _check("mop_vocab_distill_bwd",
+           lib().mop_vocab_distill_bwd(device, N, H, V, K, _ptr(X), _ptr(W_voc), _ptr(teacher_idx), _ptr(teacher_logits),
+                                       _ptr(teacher_lse), temperature, _ptr(student), _ptr(lse), _ptr(dloss), _ptr(dX),
+                                       _ptr(dW_voc), _ptr(workspace), _stream(stream)))
     return workspace
 
 

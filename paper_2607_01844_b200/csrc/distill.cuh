@@ -1,0 +1,571 @@
+// Distillation from a teacher's top logits through the vocabulary projection (Eq. 5's projection with another loss on it):
+//
+//   Y = X W_voc (never stored),  s = Y / tau,  lse = log sum_v exp s_v,  q_k the teacher's probabilities of its K entries
+//   loss[n] = sum_k q_k (log q_k - s[n, i_k] + lse[n])
+//   dY[n,v] = dloss[n] / tau (Q p[n,v] - sum_{k: i_k = v} q_k),   p = exp(s - lse),   Q = sum_k q_k
+//
+// vd_gemm_kernel runs three products on CTA pairs (256 x 256 tiles, tcgen05.mma.cta_group::2, six stages of 64 of K, as
+// tc_gemm2_kernel), with eight epilogue warps:
+//   VD_L  Y = X W_voc: per row and 128 columns the maximum and the sum of exponentials, and the logits of the teacher's entries
+//   VD_P  dY, one block of vocabulary columns, bf16 (the only piece of the N x V matrix that ever exists)
+//   VD_W  dW_voc[:, block] = X^T dY, bf16
+// and dX += dY W_voc^T runs on tc_gemm2_kernel<TC_VX>, beside VD_W.
+//
+// A row's entries are sorted by column first (distill_prep_kernel), so that the thread that owns the row finds those of its 128
+// columns by one binary search while the tile is being multiplied.
+#pragma once
+#include <limits.h>
+
+#include "gemm_tc2.cuh"
+
+namespace mop {
+
+enum : int { VD_L = 0, VD_P = 1, VD_W = 2 };
+
+constexpr int VD_STAGES = 6;
+constexpr int VD_EPI_WARPS = 8;
+constexpr int VD_THREADS = 64 + 32 * VD_EPI_WARPS;
+constexpr int VD_BOX_BYTES = 128 * 64 * 2;                    // store box: 128 rows x 64 bf16 columns, one for each column half
+constexpr int VD_SMEM_BYTES = VD_STAGES * T2_STAGE_BYTES + 2 * VD_BOX_BYTES + 1024 /*align*/ + TC_BAR_BYTES;
+// K blocks (of 64) per accumulation segment of the forward.  The tensor core truncates where it adds; a segment starts from zero and
+// the finished ones are added in fp32 registers, rounding to nearest.
+constexpr int VD_SEG = 4;
+constexpr int VD_MAX_K = 256;                                 // entries of a teacher's list
+
+struct VdArgs {
+    int N, H, V, K;               // tokens, hidden size, vocabulary, entries per token
+    int tiles_m, tiles_n, n_group, kblocks;
+    int n_base;                   // VD_P: first vocabulary column of the block
+    int cols;                     // VD_L, VD_P: columns of the whole matrix that exist (V)
+    int a_split, b_split;         // that operand's columns are no multiple of 64: one copy per 64-wide chunk, whose edge is zero-filled
+    float c;                      // log2(e) / tau
+    const int32_t* scol;          // [N, K] columns of the entries, ascending (INT_MAX: none)
+    const int32_t* sslot;         // VD_L: the place of each in the caller's list
+    const float* sval;            // VD_P: dY of each
+    float* student;               // VD_L: [N, K] logits at the entries
+    float2* part;                 // VD_L: [2 tiles_n][N] (maximum, sum)
+    const float* coef;            // VD_P: dloss / tau Q per row
+    const float* lse2;            // VD_P: log-sum-exp per row in units of log 2
+    int32_t* status;
+    bool gemm_follows;
+    PdlNote note;
+};
+
+__device__ __forceinline__ float ex2(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+
+// First of the row's sorted columns that is not below `col`.
+__device__ __forceinline__ int vd_first(const int32_t* __restrict__ row, int K, int col) {
+    int lo = 0, hi = K;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (__ldg(row + mid) < col) lo = mid + 1; else hi = mid;
+    }
+    return lo;
+}
+
+template <int KIND>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VD_THREADS, 1)
+vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO,
+               const VdArgs args) {
+    constexpr int S = VD_STAGES;
+    constexpr bool A_MN = KIND == VD_W;                       // the tokens are K: X^T lies with M contiguous
+    extern __shared__ uint8_t tc_smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tc_smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* boxes = smem + S * T2_STAGE_BYTES;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(boxes + 2 * VD_BOX_BYTES);
+    // bars: [0,S) full (leader's are used), [S,2S) empty (both), tmem_full[2] (both), tmem_empty[2] (leader's)
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * S + 4);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int warp = warp_index(), lane = threadIdx.x % 32;
+    const uint32_t rank = cluster_ctarank();
+    const bool leader = rank == 0;
+    const uint32_t smem_base = smem_u32(smem);
+    const uint32_t bar_base = smem_u32(bars);
+    auto full_bar = [&](int s) { return bar_base + 8u * s; };
+    auto empty_bar = [&](int s) { return bar_base + 8u * (S + s); };
+    auto tfull_bar = [&](int b) { return bar_base + 8u * (2 * S + b); };
+    auto tempty_bar = [&](int b) { return bar_base + 8u * (2 * S + 2 + b); };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * VD_EPI_WARPS); }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        tma_prefetch_desc(&tmA); tma_prefetch_desc(&tmB);
+        if (KIND != VD_L) tma_prefetch_desc(&tmO);
+    }
+    if (warp == 1) tmem2_alloc(smem_u32(tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();          // the peer's barriers exist before anything signals them
+    tc_fence_after();
+    const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    pdl_begin_gemm(args.gemm_follows, args.note);
+
+    const int total = args.tiles_m * args.tiles_n, nkb = args.kblocks;
+    const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+    // blocks of n_group n-tiles, row tiles slower inside one: the pairs that run at the same time cover a nearly square patch
+    auto decode = [&](int t, int& mt, int& nt) {
+        const int per = args.n_group * args.tiles_m, g = t / per, r = t - g * per;
+        const int w = min(args.n_group, args.tiles_n - g * args.n_group);
+        mt = r / w;
+        nt = g * args.n_group + r - mt * w;
+    };
+
+    if (warp == 0) {
+        // ===================================================================== TMA producer (both CTAs)
+        const bool el = elect_one();
+        int stage = 0; uint32_t phase = 0; bool alive = true;
+        for (int t = cluster_id; t < total && alive; t += n_clusters) {
+            int mt, nt;
+            decode(t, mt, nt);
+            const int m0 = 256 * mt + 128 * (int)rank, n0 = args.n_base + 256 * nt + 128 * (int)rank;
+            for (int kb = 0; kb < nkb; ++kb) {
+                if (!mbar_wait_all(empty_bar(stage), phase ^ 1u, abort_flag, args.status, STATUS_WAIT_EMPTY)) { alive = false; break; }
+                const uint32_t fb = full_bar(stage) & T2_PEER_MASK;    // the leader's barrier
+                const uint32_t sA = smem_base + stage * T2_STAGE_BYTES, sB = sA + T2_A_BYTES;
+                const int k0 = kb * TC_BK;
+                if (el) {
+                    if (leader) mbar_expect_tx(full_bar(stage), 2 * T2_STAGE_BYTES);
+                    if constexpr (!A_MN) tma2_load_2d(sA, &tmA, fb, k0, m0);
+                    else if (!args.a_split) tma2_load_3d(sA, &tmA, fb, 0, k0, m0 >> 6);
+                    else {
+                        tma2_load_2d(sA, &tmA, fb, m0, k0);
+                        tma2_load_2d(sA + TC_CHUNK_BYTES, &tmA, fb, m0 + 64, k0);
+                    }
+                    if (!args.b_split) tma2_load_3d(sB, &tmB, fb, 0, k0, n0 >> 6);
+                    else {
+                        tma2_load_2d(sB, &tmB, fb, n0, k0);
+                        tma2_load_2d(sB + TC_CHUNK_BYTES, &tmB, fb, n0 + 64, k0);
+                    }
+                }
+                if (++stage == S) { stage = 0; phase ^= 1u; }
+            }
+        }
+    } else if (warp == 1) {
+        // ===================================================================== MMA issuer (leader CTA)
+        if (leader) {
+            const bool el = elect_one();
+            constexpr uint32_t idesc = make_idesc2(A_MN, true);
+            const uint64_t desc_a = A_MN ? smem_desc(0, TC_CHUNK_BYTES, 1024) : smem_desc(0, 0, 1024);
+            const uint64_t desc_b = smem_desc(0, TC_CHUNK_BYTES, 1024);
+            constexpr uint32_t a_step = (A_MN ? 2048 : 32) >> 4, b_step = 2048 >> 4;
+            int stage = 0; uint32_t phase = 0; int it = 0; bool alive = true;
+            for (int t = cluster_id; t < total && alive; t += n_clusters) {
+                uint32_t d_tmem = 0;
+                int kseg = 0;                            // K block inside the segment
+                for (int kb = 0; kb < nkb; ++kb) {
+                    if (kb == 0 || (KIND == VD_L && kseg == VD_SEG)) {
+                        if (kb) {                        // segment done: the epilogue adds it up, the next one goes to the other accumulator
+                            if (el) umma2_commit_both(tfull_bar(it & 1));
+                            ++it;
+                            kseg = 0;
+                        }
+                        if (!mbar_wait_all(tempty_bar(it & 1), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, args.status,
+                                           STATUS_WAIT_TMEM_EMPTY)) { alive = false; break; }
+                        tc_fence_after();
+                        d_tmem = tmem_base + (uint32_t)(it & 1) * TC_BN;
+                    }
+                    if (!mbar_wait_all(full_bar(stage), phase, abort_flag, args.status, STATUS_WAIT_FULL)) { alive = false; break; }
+                    tc_fence_after();
+                    const uint32_t sA = smem_base + stage * T2_STAGE_BYTES;
+                    const uint64_t da = desc_a | (uint64_t)((sA & 0x3ffffu) >> 4);
+                    const uint64_t db = desc_b | (uint64_t)(((sA + T2_A_BYTES) & 0x3ffffu) >> 4);
+                    if (el) {
+#pragma unroll
+                        for (int k4 = 0; k4 < TC_BK / 16; ++k4)
+                            umma2_bf16(d_tmem, da + k4 * a_step, db + k4 * b_step, idesc, (kseg | k4) != 0 ? 1u : 0u);
+                        umma2_commit_both(empty_bar(stage));
+                    }
+                    ++kseg;
+                    if (++stage == S) { stage = 0; phase ^= 1u; }
+                }
+                if (!alive) break;
+                if (el) umma2_commit_both(tfull_bar(it & 1));
+                ++it;
+            }
+        }
+    } else {
+        // ===================================================================== epilogue (8 warps, both CTAs)
+        const int quarter = warp & 3;            // TMEM lanes 32*quarter .. +31 belong to this warp
+        const int half = (warp - 2) >> 2;        // columns [128*half, 128*half + 128) of the tile
+        const uint32_t ta0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * 128;
+        int it = 0;
+        bool ok = true;
+        for (int t = cluster_id; t < total && ok; t += n_clusters) {
+            int mt, nt;
+            decode(t, mt, nt);
+            const int row = 256 * mt + 128 * (int)rank + quarter * 32 + lane;
+            const int col0 = args.n_base + 256 * nt + 128 * half;         // vocabulary column of this thread's first
+            if constexpr (KIND == VD_L) {
+                const bool mine = row < args.N;
+                const int32_t* list = args.scol + (size_t)row * args.K;
+                int at = mine ? vd_first(list, args.K, col0) : args.K;
+                int next = at < args.K ? __ldg(list + at) : INT_MAX;
+                float y[4][32];
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) y[g][i] = 0.0f;
+                const int nseg = (nkb + VD_SEG - 1) / VD_SEG;
+                for (int sg = 0; sg < nseg; ++sg) {
+                    if (!mbar_wait_warp(tfull_bar(it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, args.status, STATUS_WAIT_TMEM_FULL,
+                                        lane)) { ok = false; break; }
+                    tc_fence_after();
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        float part[32];
+                        tmem_ld32(ta0 + (uint32_t)(it & 1) * TC_BN + 32 * g, part);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) y[g][i] += part[i];
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(tempty_bar(it & 1) & T2_PEER_MASK);
+                    ++it;
+                }
+                if (!ok) break;
+                float m = -INFINITY, sum = 0.0f;
+                if (col0 + 128 > args.cols) {             // the vocabulary ends inside these columns
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (col0 + 32 * g + i >= args.cols) y[g][i] = -INFINITY;
+                }
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) m = fmaxf(m, y[g][i]);
+                const float mc = m == -INFINITY ? 0.0f : m * args.c;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) sum += ex2(fmaf(y[g][i], args.c, -mc));
+                    while (next < col0 + 32 * (g + 1)) {  // (entries lie inside the vocabulary)
+                        const int i = next - col0 - 32 * g;
+                        float v = 0.0f;
+#pragma unroll
+                        for (int q = 0; q < 32; ++q) v = i == q ? y[g][q] : v;
+                        args.student[(size_t)row * args.K + __ldg(args.sslot + (size_t)row * args.K + at)] = v;
+                        ++at;
+                        next = at < args.K ? __ldg(list + at) : INT_MAX;
+                    }
+                }
+                if (mine) args.part[(size_t)(2 * nt + half) * args.N + row] = make_float2(m, sum);
+            } else {
+                const bool mine = row < args.N;
+                float coef = 0.0f, lse2 = 0.0f;
+                int at = args.K, next = INT_MAX;
+                const int32_t* list = args.scol + (size_t)row * args.K;
+                if constexpr (KIND == VD_P) {
+                    if (mine) {
+                        coef = args.coef[row];
+                        lse2 = args.lse2[row];
+                        at = vd_first(list, args.K, col0);
+                        next = at < args.K ? __ldg(list + at) : INT_MAX;
+                    }
+                }
+                bool ready = mbar_wait_warp(tfull_bar(it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, args.status, STATUS_WAIT_TMEM_FULL, lane);
+                // the four warps of a column half meet at named barriers below: they give up together or not at all
+                if (!bar_vote_all(1 + half, 128, ready)) { ok = false; break; }
+                tc_fence_after();
+                float y[4][32];
+                const uint32_t ta = ta0 + (uint32_t)(it & 1) * TC_BN;
+                tmem_ld32_nowait(ta, y[0]);
+                tmem_ld32_nowait(ta + 32, y[1]);
+                tmem_ld32_nowait(ta + 64, y[2]);
+                tmem_ld32_nowait(ta + 96, y[3]);
+                tmem_ld_wait4(y[0], y[1], y[2], y[3]);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(tempty_bar(it & 1) & T2_PEER_MASK);
+                ++it;
+                uint8_t* box = boxes + half * VD_BOX_BYTES;
+                uint8_t* rowp = box + (quarter * 32 + lane) * 128;
+                const bool issuer = quarter == 0 && lane == 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {             // 64 columns at a time: a box of 128-byte rows, 16-byte chunks swizzled by row
+                    if constexpr (KIND == VD_P)
+#pragma unroll
+                        for (int g = 2 * h; g < 2 * h + 2; ++g)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) y[g][i] = coef * ex2(fmaf(y[g][i], args.c, -lse2));
+                    if (issuer) tma_store_wait_read<0>(); // the box's last copy has been read
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float* v = &y[2 * h + j / 4][(j % 4) * 8];
+                        *reinterpret_cast<uint4*>(rowp + ((j ^ (lane & 7)) << 4)) =
+                            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+                    }
+                    if constexpr (KIND == VD_P)
+                        while (next < col0 + 64 * (h + 1)) {              // the teacher's entries among these columns
+                            const int i = next - col0 - 64 * h;
+                            const float v = __ldg(args.sval + (size_t)row * args.K + at);
+                            *reinterpret_cast<bf16*>(rowp + (((i >> 3) ^ (lane & 7)) << 4) + (i & 7) * 2) = __float2bfloat16_rn(v);
+                            ++at;
+                            next = at < args.K ? __ldg(list + at) : INT_MAX;
+                        }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+                    if (issuer) {
+                        const int x = 256 * nt + 128 * half + 64 * h, r0 = 256 * mt + 128 * (int)rank;
+                        if (x < args.cols && r0 < (KIND == VD_P ? args.N : args.H)) tma_store_2d(&tmO, smem_u32(box), x, r0);
+                        tma_store_commit();
+                    }
+                }
+            }
+        }
+        if (KIND != VD_L && quarter == 0 && lane == 0) tma_store_wait_all();       // boxes read, and written, before the CTA exits
+    }
+
+    // ------------------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000ll) __nanosleep(1000);
+        __syncthreads();
+    }
+    cluster_sync_all();          // neither CTA leaves while the other may still signal its barriers
+    if (warp == 1) {
+        tc_fence_after();
+        tmem2_dealloc(tmem_base, 512);
+    }
+}
+
+// ------------------------------------------------------------------------------------------ the teacher's lists
+struct DistillLists {
+    const int32_t* idx; const float* logits; const float* lse;      // the caller's: [N,K], [N,K], [N] or null
+    int N, V, K;
+    float tau;
+};
+// Teacher's probabilities of the entries lane + 32 j of row n (0 where there is none), and log q; a row without entries has none.
+template <int J>
+__device__ __forceinline__ void distill_teacher(const DistillLists& l, size_t n, int lane, int32_t (&col)[J], float (&q)[J], float (&logq)[J]) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        const int k = lane + 32 * j;
+        col[j] = INT_MAX;
+        logq[j] = -INFINITY;
+        if (k < l.K) {
+            const int32_t v = l.idx[n * l.K + k];
+            if (v >= 0 && v < l.V) { col[j] = v; logq[j] = __fdiv_rn(l.logits[n * l.K + k], l.tau); }
+        }
+        m = fmaxf(m, logq[j]);
+    }
+    float norm = 0.0f;
+    if (l.lse) {
+        norm = l.lse[n];
+    } else {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (m == -INFINITY) m = 0.0f;
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) s += expf(logq[j] - m);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        norm = s == 0.0f ? 0.0f : m + logf(s);
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+        if (col[j] != INT_MAX) logq[j] -= norm;
+        q[j] = col[j] != INT_MAX ? expf(logq[j]) : 0.0f;
+    }
+}
+
+struct DistillPrep {
+    DistillLists l;
+    int32_t* scol; int32_t* sslot; float* sval;                     // sslot forward, sval backward
+    float* student_out;                                             // forward: entries outside the vocabulary get 0
+    const float* student; const float* lse; const float* dloss;     // backward
+    float* coef; float* lse2;
+    int4* tiles; int32_t* n_tiles; int32_t* status;                 // as in vocab_setup_kernel
+};
+constexpr int DP_WARPS = 8;
+// A warp per row: places every entry by counting the smaller ones (equal columns by their place).  Backward: dY of each entry, the
+// probabilities of equal columns added up, so that every one of them holds the same value.
+template <int J, bool BWD>
+__global__ void __launch_bounds__(32 * DP_WARPS) distill_prep_kernel(const DistillPrep a) {
+    pdl_begin();
+    __shared__ int32_t scols[DP_WARPS][VD_MAX_K];
+    __shared__ float sq[DP_WARPS][BWD ? VD_MAX_K : 1];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, N = a.l.N, K = a.l.K;
+    if (blockIdx.x == 0) {
+        const int nt = (N + 255) / 256;
+        for (int i = threadIdx.x; i < nt; i += blockDim.x) a.tiles[i] = make_int4(0, 256 * i, min(256, N - 256 * i), 0);
+        if (threadIdx.x == 0) { *a.n_tiles = nt; *a.status = 0; a.status[VOCAB_NOTE] = 0; }
+    }
+    for (int n = blockIdx.x * DP_WARPS + warp; n < N; n += gridDim.x * DP_WARPS) {
+        int32_t col[J];
+        float q[J], logq[J];
+        float total = 0.0f;
+        if constexpr (BWD) {
+            distill_teacher<J>(a.l, n, lane, col, q, logq);
+#pragma unroll
+            for (int j = 0; j < J; ++j) total += q[j];
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        } else {
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int k = lane + 32 * j;
+                const int32_t v = k < K ? a.l.idx[(size_t)n * K + k] : -1;
+                col[j] = v >= 0 && v < a.l.V ? v : INT_MAX;
+                if (k < K && col[j] == INT_MAX) a.student_out[(size_t)n * K + k] = 0.0f;
+            }
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int k = lane + 32 * j;
+            if (k < K) { scols[warp][k] = col[j]; if constexpr (BWD) sq[warp][k] = q[j]; }
+        }
+        __syncwarp();
+        int rank[J];
+        float same[J];
+#pragma unroll
+        for (int j = 0; j < J; ++j) { rank[j] = 0; same[j] = 0.0f; }
+        for (int i = 0; i < K; ++i) {
+            const int32_t v = scols[warp][i];
+            float w = 0.0f;
+            if constexpr (BWD) w = sq[warp][i];
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const int k = lane + 32 * j;
+                rank[j] += v < col[j] || (v == col[j] && i < k) ? 1 : 0;
+                if constexpr (BWD) same[j] += v == col[j] ? w : 0.0f;
+            }
+        }
+        float g = 0.0f, lse = 0.0f;
+        if constexpr (BWD) {
+            g = __fdiv_rn(a.dloss[n], a.l.tau);
+            lse = a.lse[n];
+            if (lane == 0) { a.coef[n] = g * total; a.lse2[n] = lse * 1.4426950408889634f; }
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int k = lane + 32 * j;
+            if (k >= K) continue;
+            const size_t to = (size_t)n * K + rank[j];
+            a.scol[to] = col[j];
+            if constexpr (!BWD) a.sslot[to] = k;
+            else if (col[j] != INT_MAX) {
+                const float p = expf(__fdiv_rn(a.student[(size_t)n * K + k], a.l.tau) - lse);
+                a.sval[to] = g * fmaf(total, p, -same[j]);
+            }
+        }
+    }
+}
+
+// lse of a row from its (maximum, sum) pairs, then the loss.  A block owns 32 rows (a lane each, its eight warps every eighth pair, as
+// vocab_lse_merge_kernel), then a warp takes four of them, lanes over the entries.
+struct DistillMerge {
+    DistillLists l;
+    const float2* part; int parts;
+    const float* student;
+    float c;
+    float *loss, *lse;
+};
+template <int J>
+__global__ void __launch_bounds__(32 * LSE_WARPS) distill_merge_kernel(const DistillMerge a) {
+    pdl_begin();
+    __shared__ float2 sh[LSE_WARPS][32];
+    __shared__ float slse[32];
+    const int N = a.l.N, K = a.l.K;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, n = blockIdx.x * 32 + lane;
+    float M = -INFINITY, S = 0.0f;
+    if (n < N) {
+#pragma unroll 4
+        for (int i = warp; i < a.parts; i += LSE_WARPS) M = fmaxf(M, a.part[(size_t)i * N + n].x);
+        const float Mc = M == -INFINITY ? 0.0f : M * a.c;
+#pragma unroll 4
+        for (int i = warp; i < a.parts; i += LSE_WARPS) {
+            const float2 q = a.part[(size_t)i * N + n];
+            S += q.y * exp2f(q.x == -INFINITY ? -INFINITY : fmaf(q.x, a.c, -Mc));
+        }
+    }
+    sh[warp][lane] = make_float2(M, S);
+    __syncthreads();
+    if (warp == 0) {
+        float m = sh[0][lane].x;
+#pragma unroll
+        for (int w = 1; w < LSE_WARPS; ++w) m = fmaxf(m, sh[w][lane].x);
+        const float mc = m == -INFINITY ? 0.0f : m * a.c;
+        float t = 0.0f;
+#pragma unroll
+        for (int w = 0; w < LSE_WARPS; ++w)
+            if (w < a.parts) t += sh[w][lane].y * exp2f(sh[w][lane].x == -INFINITY ? -INFINITY : fmaf(sh[w][lane].x, a.c, -mc));
+        const float l = __fdiv_rn(m, a.l.tau) + logf(t);
+        slse[lane] = l;
+        if (n < N) a.lse[n] = l;
+    }
+    __syncthreads();
+    for (int r = warp; r < 32; r += LSE_WARPS) {
+        const int row = blockIdx.x * 32 + r;
+        if (row >= N) break;
+        int32_t col[J];
+        float q[J], logq[J], sum = 0.0f;
+        distill_teacher<J>(a.l, row, lane, col, q, logq);
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (q[j] != 0.0f) sum += q[j] * (logq[j] - __fdiv_rn(a.student[(size_t)row * K + lane + 32 * j], a.l.tau) + slse[r]);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (lane == 0) a.loss[row] = sum;
+    }
+}
+
+// dX from its fp32 sums [N, pitch], 8 elements a thread.
+__global__ void __launch_bounds__(256) distill_dx_kernel(const float* __restrict__ src, bf16* __restrict__ dst, int N, int H, int pitch) {
+    pdl_begin();
+    const int per = H / 8;
+    const size_t n8 = (size_t)N * per;
+    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < n8; i += (size_t)gridDim.x * blockDim.x) {
+        const size_t r = i / per, c = (i - r * per) * 8;
+        const float4 a = *reinterpret_cast<const float4*>(src + r * pitch + c), b = *reinterpret_cast<const float4*>(src + r * pitch + c + 4);
+        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        store_bf16_run<8>(dst + r * H + c, v);
+    }
+}
+
+// ------------------------------------------------------------------------------------------ host
+template <int KIND>
+inline mop_status vd_set_smem() {
+    return cudaFuncSetAttribute(vd_gemm_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, VD_SMEM_BYTES) == cudaSuccess
+               ? MOP_OK : MOP_ERR_CUDA;
+}
+inline mop_status vd_init() {
+    mop_status r;
+    if ((r = vd_set_smem<VD_L>()) != MOP_OK) return r;
+    if ((r = vd_set_smem<VD_P>()) != MOP_OK) return r;
+    return vd_set_smem<VD_W>();
+}
+template <int KIND>
+inline mop_status vd_launch(const TcPlan* p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const VdArgs& args,
+                            cudaStream_t st) {
+    return pdl_launch(vd_gemm_kernel<KIND>, p->sm_count & ~1, VD_THREADS, VD_SMEM_BYTES, st, a, b, o, args) == cudaSuccess ? MOP_OK
+                                                                                                                      : MOP_ERR_CUDA;
+}
+// 2-D map over `cols` columns of a bf16 matrix whose rows are `pitch` elements apart, for stores; box = {64 columns, 128 rows}.
+inline bool vd_map_out(const TcPlan* p, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch) {
+    return tc_map_2d_pitch(p, m, base, rows, cols, pitch, 128);
+}
+
+#define DISTILL_BY_K(K, GO)                                       \
+    do {                                                          \
+        if ((K) <= 32) GO(1);                                     \
+        else if ((K) <= 64) GO(2);                                \
+        else if ((K) <= 128) GO(4);                               \
+        else GO(8);                                               \
+    } while (0)
+
+}  // namespace mop

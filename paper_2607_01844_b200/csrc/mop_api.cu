@@ -15,6 +15,7 @@
 #include "gemm_rs.cuh"
 #include "route_permute.cuh"
 #include "balance.cuh"
+#include "distill.cuh"
 
 using namespace mop;
 
@@ -1608,6 +1609,7 @@ mop_status vocab_plan(int device, TcPlan** out) {
         mop_moe_shape dummy{};
         mop_status r = tc_plan_init(p, dummy, prop.multiProcessorCount, &g_vocab_prof);
         if (r == MOP_OK) r = tc2_init();
+        if (r == MOP_OK) r = vd_init();
         if (r != MOP_OK) return r;
         g_vocab_ready[device] = true;
     }
@@ -1797,6 +1799,178 @@ mop_status mop_vocab_loss_bwd(int device, int32_t N, int32_t H, int32_t V, const
     const size_t cap = (size_t)p->sm_count * 16;
     pdl_launch(f32_to_bf16_kernel, (unsigned)((n8 + 255) / 256 < cap ? (n8 + 255) / 256 : cap), 256, 0, st,
                reinterpret_cast<const float4*>(dx32), static_cast<uint4*>(dX), n8);
+    return cudaGetLastError() == cudaSuccess ? MOP_OK : MOP_ERR_CUDA;
+}
+
+// ---------------------------------------------------------------------------------------------
+// Distillation from a teacher's top logits through the same projection
+// ---------------------------------------------------------------------------------------------
+namespace {
+struct DistillLayout { size_t status, tiles, scol, sslot, sval, coef, lse2, part, dy, dx32, total; int vc, hp; };
+DistillLayout distill_layout(int N, int H, int V, int K, bool backward) {
+    DistillLayout L{};
+    size_t o = 0;
+    auto take = [&](size_t b) { size_t r = o; o += align_up(b); return r; };
+    L.status = take(256);                 // first: mop_vocab_poll reads it without knowing the shape
+    L.tiles = take(tc_tile_table_bytes(N, 1));
+    L.scol = take((size_t)N * K * 4);
+    if (!backward) {
+        L.sslot = take((size_t)N * K * 4);
+        L.part = take((size_t)ceil_div(V, 256) * 2 * N * 8);
+    } else {
+        L.vc = V < kVocabBlock ? ceil_div(V, 64) * 64 : kVocabBlock;
+        L.hp = ceil_div(H, 32) * 32;      // dX is added up in whole runs of 32 columns
+        L.sval = take((size_t)N * K * 4);
+        L.coef = take((size_t)N * 4);
+        L.lse2 = take((size_t)N * 4);
+        L.dy = take((size_t)N * L.vc * 2);
+        L.dx32 = take((size_t)N * L.hp * 4);
+    }
+    L.total = o;
+    return L;
+}
+mop_status distill_check(int device, int32_t N, int32_t H, int32_t V, int32_t K, float temperature) {
+    if (N < 0 || H < 1 || V < 1 || K < 1 || !(temperature > 0.0f) || !(temperature < INFINITY)) return MOP_ERR_INVALID_ARG;
+    if (device < 0 || device >= kMaxDevices) return MOP_ERR_INVALID_ARG;
+    if (H % 8 || V % 8) return MOP_ERR_ALIGN;
+    if (K > VD_MAX_K || (long long)N * 2 >= (1ll << 31) || (long long)H * V >= (1ll << 40)) return MOP_ERR_SHAPE;
+    return MOP_OK;
+}
+bool distill_sizes_ok(int32_t N, int32_t H, int32_t V, int32_t K) { return distill_check(0, N, H, V, K, 1.0f) == MOP_OK; }
+// W_voc (or X, transposed) as an operand with its columns contiguous: 64-wide chunks, two in a copy where there are only whole ones.
+bool distill_map_mn(const TcPlan* p, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols) {
+    return tc_map_mn(p, m, base, rows, cols, 2);
+}
+}  // namespace
+
+size_t mop_vocab_distill_workspace_bytes(int32_t N, int32_t H, int32_t V, int32_t K) {
+    return distill_sizes_ok(N, H, V, K) ? distill_layout(N, H, V, K, false).total : 0;
+}
+size_t mop_vocab_distill_bwd_workspace_bytes(int32_t N, int32_t H, int32_t V, int32_t K) {
+    return distill_sizes_ok(N, H, V, K) ? distill_layout(N, H, V, K, true).total : 0;
+}
+
+mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, int32_t K, const void* X, const void* W_voc,
+                                 const int32_t* teacher_idx, const float* teacher_logits, const float* teacher_lse_opt,
+                                 float temperature, float* loss, float* student, float* lse, void* workspace, void* stream) {
+    mop_status r = distill_check(device, N, H, V, K, temperature);
+    if (r != MOP_OK) return r;
+    if (N == 0) return MOP_OK;
+    if (!X || !W_voc || !teacher_idx || !teacher_logits || !loss || !student || !lse || !workspace) return MOP_ERR_INVALID_ARG;
+    if (!aligned16(X) || !aligned16(W_voc) || !aligned16(teacher_idx) || !aligned16(teacher_logits) || !aligned16(teacher_lse_opt) ||
+        !aligned16(loss) || !aligned16(student) || !aligned16(lse) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
+        return MOP_ERR_ALIGN;
+    DeviceGuard guard(device);
+    if (!guard.ok) return MOP_ERR_CUDA;
+    TcPlan* p = nullptr;
+    if ((r = vocab_plan(device, &p)) != MOP_OK) return r;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const DistillLayout L = distill_layout(N, H, V, K, false);
+    char* w = static_cast<char*>(workspace);
+    int32_t* tiles = reinterpret_cast<int32_t*>(w + L.tiles);
+    CUtensorMap mX, mW;
+    if (!tc_map_2d(p, &mX, X, N, H, 128) || !distill_map_mn(p, &mW, W_voc, H, V)) return MOP_ERR_CUDA;
+    const DistillLists lists = {teacher_idx, teacher_logits, teacher_lse_opt, N, V, K, temperature};
+    DistillPrep a{};
+    a.l = lists; a.scol = reinterpret_cast<int32_t*>(w + L.scol); a.sslot = reinterpret_cast<int32_t*>(w + L.sslot);
+    a.student_out = student;
+    a.tiles = reinterpret_cast<int4*>(tiles + 64); a.n_tiles = tiles; a.status = reinterpret_cast<int32_t*>(w + L.status);
+    const int blocks = min(ceil_div(N, DP_WARPS), p->sm_count * 8);
+#define GO(J) pdl_launch(distill_prep_kernel<J, false>, blocks, 32 * DP_WARPS, 0, st, a)
+    DISTILL_BY_K(K, GO);
+#undef GO
+    VdArgs g{};
+    g.N = N; g.H = H; g.V = V; g.K = K;
+    g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(V, 256); g.n_group = VOCAB_N_GROUP; g.kblocks = ceil_div(H, TC_BK);
+    g.cols = V; g.b_split = V % 64 != 0; g.c = (float)(1.4426950408889634 / temperature);
+    g.scol = a.scol; g.sslot = a.sslot; g.student = student; g.part = reinterpret_cast<float2*>(w + L.part);
+    g.status = a.status;
+    if ((r = vd_launch<VD_L>(p, mX, mW, mW, g, st)) != MOP_OK) return r;
+    DistillMerge m{};
+    m.l = lists; m.part = g.part; m.parts = 2 * g.tiles_n; m.student = student; m.c = g.c; m.loss = loss; m.lse = lse;
+#define GO(J) pdl_launch(distill_merge_kernel<J>, ceil_div(N, 32), 32 * LSE_WARPS, 0, st, m)
+    DISTILL_BY_K(K, GO);
+#undef GO
+    return cudaGetLastError() == cudaSuccess ? MOP_OK : MOP_ERR_CUDA;
+}
+
+mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, int32_t K, const void* X, const void* W_voc,
+                                 const int32_t* teacher_idx, const float* teacher_logits, const float* teacher_lse_opt,
+                                 float temperature, const float* student, const float* lse, const float* dloss, void* dX,
+                                 void* dW_voc, void* workspace, void* stream) {
+    mop_status r = distill_check(device, N, H, V, K, temperature);
+    if (r != MOP_OK) return r;
+    if (!W_voc || !dW_voc || !workspace) return MOP_ERR_INVALID_ARG;
+    if (N > 0 && (!X || !teacher_idx || !teacher_logits || !student || !lse || !dloss || !dX)) return MOP_ERR_INVALID_ARG;
+    if (!aligned16(X) || !aligned16(W_voc) || !aligned16(teacher_idx) || !aligned16(teacher_logits) || !aligned16(teacher_lse_opt) ||
+        !aligned16(student) || !aligned16(lse) || !aligned16(dloss) || !aligned16(dX) || !aligned16(dW_voc) ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255u))
+        return MOP_ERR_ALIGN;
+    DeviceGuard guard(device);
+    if (!guard.ok) return MOP_ERR_CUDA;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (N == 0) {   // no tokens: the weight gradient is zero
+        CUDA_OK(cudaMemsetAsync(dW_voc, 0, (size_t)H * V * 2, st));
+        return MOP_OK;
+    }
+    TcPlan* p = nullptr;
+    if ((r = vocab_plan(device, &p)) != MOP_OK) return r;
+    const DistillLayout L = distill_layout(N, H, V, K, true);
+    char* w = static_cast<char*>(workspace);
+    int32_t* tiles = reinterpret_cast<int32_t*>(w + L.tiles);
+    int32_t* status = reinterpret_cast<int32_t*>(w + L.status);
+    bf16* dY = reinterpret_cast<bf16*>(w + L.dy);
+    float* dx32 = reinterpret_cast<float*>(w + L.dx32);
+    CUtensorMap mX, mXT, mWn, mWk;
+    if (!tc_map_2d(p, &mX, X, N, H, 128) || !distill_map_mn(p, &mXT, X, N, H) || !distill_map_mn(p, &mWn, W_voc, H, V) ||
+        !tc_map_3d(p, &mWk, W_voc, 1, H, V, 128))
+        return MOP_ERR_CUDA;
+    DistillPrep a{};
+    a.l = {teacher_idx, teacher_logits, teacher_lse_opt, N, V, K, temperature};
+    a.scol = reinterpret_cast<int32_t*>(w + L.scol); a.sval = reinterpret_cast<float*>(w + L.sval);
+    a.student = student; a.lse = lse; a.dloss = dloss;
+    a.coef = reinterpret_cast<float*>(w + L.coef); a.lse2 = reinterpret_cast<float*>(w + L.lse2);
+    a.tiles = reinterpret_cast<int4*>(tiles + 64); a.n_tiles = tiles; a.status = status;
+    const int blocks = min(ceil_div(N, DP_WARPS), p->sm_count * 8);
+#define GO(J) pdl_launch(distill_prep_kernel<J, true>, blocks, 32 * DP_WARPS, 0, st, a)
+    DISTILL_BY_K(K, GO);
+#undef GO
+    for (int c0 = 0; c0 < V; c0 += L.vc) {
+        const int cw = V - c0 < L.vc ? V - c0 : L.vc, cw64 = ceil_div(cw, 64) * 64;
+        CUtensorMap mdYk, mdYn, mdYo, mdW;
+        if (!tc_map_2d_pitch(p, &mdYk, dY, N, cw, L.vc, 128) || !tc_map_chunked_2d_pitch(p, &mdYn, dY, N, cw64, L.vc, 2) ||
+            !vd_map_out(p, &mdYo, dY, N, L.vc, L.vc) || !vd_map_out(p, &mdW, static_cast<bf16*>(dW_voc) + c0, H, cw, V))
+            return MOP_ERR_CUDA;
+        const PdlNote note = {status + VOCAB_NOTE, c0 / L.vc + 1};
+        VdArgs base{};
+        base.N = N; base.H = H; base.V = V; base.K = K; base.n_group = VOCAB_N_GROUP; base.status = status; base.gemm_follows = true;
+        {   // dY block, logits formed again on the tensor cores
+            VdArgs g = base;
+            g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(cw, 256); g.kblocks = ceil_div(H, TC_BK);
+            g.n_base = c0; g.cols = cw64; g.b_split = V % 64 != 0; g.c = (float)(1.4426950408889634 / temperature);
+            g.scol = a.scol; g.sval = a.sval; g.coef = a.coef; g.lse2 = a.lse2;
+            if ((r = vd_launch<VD_P>(p, mX, mWn, mdYo, g, st)) != MOP_OK) return r;
+        }
+        {   // dW[:, block] = X^T dY (K = the N tokens), written once
+            VdArgs g = base;
+            g.tiles_m = ceil_div(H, 256); g.tiles_n = ceil_div(cw, 256); g.kblocks = ceil_div(N, TC_BK);
+            g.cols = cw; g.a_split = H % 64 != 0; g.note = note;
+            if ((r = vd_launch<VD_W>(p, mXT, mdYn, mdW, g, st)) != MOP_OK) return r;
+        }
+        {   // dX += dY W[:, block]^T in fp32 across the blocks, beside the weight gradient (as in mop_vocab_loss_bwd)
+            TcArgs g{};
+            g.n_mtiles = tiles; g.n_group = VOCAB_N_GROUP; g.mtiles = reinterpret_cast<const int4*>(tiles + 64);
+            g.E = 1; g.status = status; g.ep.M_total = N;
+            g.note = note;
+            g.gemm_follows = c0 + L.vc < V;
+            g.tiles_n = ceil_div(H, 256); g.kblocks = ceil_div(cw, TC_BK); g.N = L.hp; g.kb_base = c0;
+            g.ep.outf = dx32; g.ep.accumulate = c0 > 0 ? 1 : 0;
+            if ((r = tc2_launch<TC_VX>(p, "vocab_dgrad", mdYk, mdYk, mWk, mWk, g, st)) != MOP_OK) return r;
+        }
+    }
+    const size_t n8 = (size_t)N * (H / 8), cap = (size_t)p->sm_count * 16;
+    pdl_launch(distill_dx_kernel, (unsigned)((n8 + 255) / 256 < cap ? (n8 + 255) / 256 : cap), 256, 0, st, dx32, static_cast<bf16*>(dX), N,
+               H, L.hp);
     return cudaGetLastError() == cudaSuccess ? MOP_OK : MOP_ERR_CUDA;
 }
 

@@ -78,3 +78,61 @@ def test_masked_experts_and_tokens_add_nothing():
         assert counts.tolist() == [[1, 0, 0, 0]]
         assert np.allclose(prob, np.array([1.25, 0.25, 0.25, 0.25]) / 3)
         assert np.isfinite(oracle.balance_loss_bwd(z, None, 1, score_fn, synth.BIAS_NONE, counts, [0, 3], [1.0])).all()
+
+
+def _distill_inputs(N=9, H=6, V=23, K=5, seed=4):
+    rng = np.random.default_rng(seed)
+    X, W = synth.bits(torch.from_numpy(rng.normal(size=(N, H))).to(torch.bfloat16)), synth.bits(torch.from_numpy(rng.normal(size=(H, V))).to(torch.bfloat16))
+    ids = rng.integers(0, V, size=(N, K))
+    t = rng.normal(size=(N, K)) * 3
+    ids[1, 2:] = -1                                  # a short list
+    ids[2] = V                                       # none at all
+    ids[3, 1] = ids[3, 0]                            # a place that is named twice
+    t[4, 0] = -np.inf
+    return X, W, ids, t
+
+
+@pytest.mark.parametrize("full", [False, True], ids=["renormalised", "whole"])
+@pytest.mark.parametrize("tau", [1.0, 2.5])
+def test_distillation_against_autodiff_of_the_divergence(tau, full):
+    X, W, ids, t = _distill_inputs()
+    V = W.shape[1]
+    dloss = np.linspace(-1, 2, X.shape[0])
+    tlse = np.log(np.exp(np.where(np.isfinite(t), t, -50) / tau).sum(1) + 3.0) if full else None
+    Y = torch.as_tensor(oracle.bf16_bits_to_f64(X) @ oracle.bf16_bits_to_f64(W)).requires_grad_()
+    logp = torch.log_softmax(Y / tau, 1)
+    want = []
+    for n in range(X.shape[0]):
+        keep = [k for k in range(ids.shape[1]) if 0 <= ids[n, k] < V]
+        s = torch.as_tensor(t[n, keep] / tau)
+        logq = s - (torch.as_tensor(tlse[n]) if full else torch.logsumexp(s, 0)) if keep else s
+        q = torch.exp(logq)
+        want.append(sum((q[i] * (logq[i] - logp[n, ids[n, k]]) for i, k in enumerate(keep) if q[i] > 0), torch.zeros((), dtype=torch.float64)))
+    want = torch.stack(want)
+    (want * torch.as_tensor(dloss)).sum().backward()
+    loss, student, lse = oracle.vocab_distill(X, W, ids, t, tau, tlse)
+    assert np.allclose(loss, want.detach().numpy(), rtol=1e-12, atol=1e-13) and loss[2] == 0.0 and (full or (loss >= -1e-13).all())
+    assert np.allclose(lse, torch.logsumexp(Y / tau, 1).detach().numpy())
+    assert np.allclose(student[0], Y[0].detach().numpy()[ids[0]]) and (student[1, 2:] == 0).all()
+    dY = oracle.vocab_distill_dlogits(X, W, ids, t, tau, dloss, tlse)
+    assert np.allclose(dY, Y.grad.numpy(), rtol=1e-10, atol=1e-14) and (dY[2] == 0).all()
+
+
+def test_distillation_gradient_against_differences():
+    _, _, ids, t = _distill_inputs()
+    rng = np.random.default_rng(8)
+    Y, h, tau = rng.normal(size=(9, 23)), 1e-6, 1.7
+    eye = synth.bits(torch.eye(23).to(torch.bfloat16))
+
+    def total(Y):                                     # (the projection is not what is differentiated: X = Y, W = 1)
+        valid, q, logq = oracle._teacher(ids, t, tau, 23, None)
+        logp = Y / tau - np.log(np.exp(Y / tau).sum(1, keepdims=True))
+        return np.where(q > 0, q * (np.where(q > 0, logq, 0) - np.take_along_axis(logp, np.where(valid, ids, 0), 1)), 0).sum()
+    Yb = synth.bits(torch.from_numpy(Y).to(torch.bfloat16))
+    Y = oracle.bf16_bits_to_f64(Yb)
+    dY = oracle.vocab_distill_dlogits(Yb, eye, ids, t, tau, np.ones(9))
+    for n, v in ((0, int(ids[0, 0])), (3, int(ids[3, 0])), (5, 11), (2, 4)):
+        up, down = Y.copy(), Y.copy()
+        up[n, v] += h
+        down[n, v] -= h
+        assert abs((total(up) - total(down)) / (2 * h) - dY[n, v]) < 1e-8
