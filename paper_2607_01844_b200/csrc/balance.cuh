@@ -7,9 +7,15 @@
 // A token is a group of G lanes (four experts a lane, and again G lanes further on where E is above 128), so that a row of the
 // logits is read once, in whole vectors, and its maximum and sums are shuffles.  All sums are fp32 in a fixed order: tokens of a
 // lane, groups of a warp, warps of a block, blocks of a sequence.  Counts are integers.
+//
+// The two products of the backward have T d E multiply-adds each (60 GFLOP at T = 16384, d = 7168, E = 256) and run on the tensor cores:
+//   dW_r = x^T dz   must have fp32 accuracy: dz goes in as three bf16 pieces (24 bits), x is bf16 already (bal_dw_pair_kernel)
+//   dX = dz W_r^T   is rounded to bf16: both operands go in as fp16 (11 bits), each row scaled by its own power of two, so that
+//                   neither the size of the upstream weight nor that of the router's weights matters (vd_gemm_kernel<VD_R>)
 #pragma once
-#include "common.cuh"
-#include "epilogue.cuh"
+#include <cuda_fp16.h>
+
+#include "distill.cuh"
 
 namespace mop {
 
@@ -231,16 +237,80 @@ __global__ void __launch_bounds__(1024) balance_finish_kernel(const BalFwdArgs a
 struct BalBwdArgs {
     const float* logits; const float* bias; const int32_t* counts; const float* dloss;
     BalSeqs q; BalShape s;
-    int chunk;
-    float* dz;                            // [T, E]: the caller's dlogits, or the workspace
-    float* dbias_part;                    // [blocks][E] or null
+    int chunk, dz_blocks;
+    float* dz;                            // [T, E] fp32, or null
+    float* dbias_part;                    // [dz_blocks][E], or null
+    // for the tensor cores, each or null:
+    int Ep;                               // columns of the buffers below: E rounded up to 64, zeros behind it
+    bf16* pieces;                         // [3][T][Ep]: dz = hi + mid + lo
+    __half* dz16; float* row_scale;       // [T][Ep], [T]: dz = dz16 row_scale
+    const float* W_r; __half* w16; float* col_scale; int d;      // [d][Ep], [d]: W_r = w16 col_scale, by the blocks behind dz_blocks
+    const uint4* x; uint4* xe;            // [128][d]: the first and last 64 tokens of the sequences' range, see bal_dw_pair_kernel
 };
+constexpr int BAL_EDGE_BLOCKS = 8;        // blocks for each of the two edges of x
+inline __host__ __device__ int bal_ep(int E) { return (E + 63) / 64 * 64; }
+
+// The power of two that brings a row's largest magnitude into [2^14, 2^15), and its reciprocal; fp16 then keeps 11 bits of what is
+// within 2^-28 of that, and the products' fp32 sums cannot overflow.
+__device__ __forceinline__ void bal_scale(float amax, float& up, float& down) {
+    const int e = (int)((__float_as_uint(amax) >> 23) & 255u) - 127;
+    const int by = min(14 - e, 126);
+    up = __uint_as_float((uint32_t)(by + 127) << 23);
+    down = __uint_as_float((uint32_t)(127 - by) << 23);
+}
+__device__ __forceinline__ uint2 bal_half4(const float* v, float by) {
+    const __half2 a = __floats2half2_rn(v[0] * by, v[1] * by), b = __floats2half2_rn(v[2] * by, v[3] * by);
+    return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+}
+// A warp per row of W_r: fp16 with the row's scale.
+__device__ __forceinline__ void bal_convert_w(const BalBwdArgs& a, int block, int blocks) {
+    const int lane = threadIdx.x % 32, warps = blockDim.x / 32;
+    for (int r = block * warps + threadIdx.x / 32; r < a.d; r += blocks * warps) {
+        const float* row = a.W_r + (size_t)r * a.s.E;
+        float amax = 0.0f, up, down;
+        for (int e = lane; e < a.s.E; e += 32) amax = fmaxf(amax, fabsf(row[e]));
+        for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        bal_scale(amax, up, down);
+        for (int e = 4 * lane; e < a.Ep; e += 128) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = e + i < a.s.E ? row[e + i] : 0.0f;
+            *reinterpret_cast<uint2*>(a.w16 + (size_t)r * a.Ep + e) = bal_half4(v, up);
+        }
+        if (lane == 0) a.col_scale[r] = down;
+    }
+}
+// Blocks of 64 tokens that the range [begin, end) of the sequences covers in part only: the padding in them must not meet the
+// products (0 x NaN), so such a block is copied, with zeros in the padding's place, and read from the copy.
+__device__ __forceinline__ bool bal_dirty(int kb, int begin, int end, int T) { return kb * 64 < begin || min(kb * 64 + 64, T) > end; }
+__device__ __forceinline__ void bal_copy_edge(const BalBwdArgs& a, int edge, int block) {
+    const int begin = bal_off(a.q, 0), end = bal_off(a.q, a.q.S);
+    if (begin >= end) return;
+    const int first = begin / 64, kb = edge ? (end - 1) / 64 : first;
+    if ((edge && kb == first) || !bal_dirty(kb, begin, end, a.s.T)) return;
+    const int per = a.d / 8;
+    for (int i = block * blockDim.x + threadIdx.x; i < 64 * per; i += BAL_EDGE_BLOCKS * blockDim.x) {
+        const int t = kb * 64 + i / per;
+        a.xe[(size_t)edge * 64 * per + i] = t >= begin && t < end ? a.x[(size_t)t * per + i % per] : make_uint4(0, 0, 0, 0);
+    }
+}
+
 // dz, zero for tokens outside the sequences.  Counts are taken relative to their mean (k T_s / E, rounded): c_e - sum p c does not
 // change by a shift, and under a nearly balanced load, which this loss aims at, the difference keeps its digits.
+// The blocks behind the first dz_blocks prepare W_r and the edges of x.
 template <int NV>
 __global__ void __launch_bounds__(NV == 8 ? 256 : 512) balance_dz_kernel(const BalBwdArgs a) {
     pdl_begin();
     extern __shared__ float bal_smem[];                                   // [W][E]
+    if ((int)blockIdx.x >= a.dz_blocks) {
+        int b = (int)blockIdx.x - a.dz_blocks;
+        if (a.xe) {
+            if (b < 2 * BAL_EDGE_BLOCKS) { bal_copy_edge(a, b / BAL_EDGE_BLOCKS, b % BAL_EDGE_BLOCKS); return; }
+            b -= 2 * BAL_EDGE_BLOCKS;
+        }
+        bal_convert_w(a, b, (int)gridDim.x - a.dz_blocks - (a.xe ? 2 * BAL_EDGE_BLOCKS : 0));
+        return;
+    }
     const BalShape s = a.s;
     const int W = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int tpw = 32 / s.G, in_group = lane % s.G, group = lane / s.G, e0 = 4 * in_group;
@@ -277,15 +347,54 @@ __global__ void __launch_bounds__(NV == 8 ? 256 : 512) balance_dz_kernel(const B
             dot = fmaf(z[i], c[i], dot);
         }
         dot = bal_sum(dot, s.G);
+        float amax = 0.0f;
 #pragma unroll
         for (int i = 0; i < 4 * NV; ++i) {
-            const int e = e0 + 4 * s.G * (i / 4) + i % 4;
             float v = w * z[i] * (c[i] - dot);
             if (s.score_fn != 0) v *= oms[i];
-            if (!on) v = 0.0f;
-            if (t < c1 && e < s.E) a.dz[(size_t)t * s.E + e] = v;
-            acc[i] += e < s.E && t < c1 ? v : 0.0f;
+            const bool there = on && e0 + 4 * s.G * (i / 4) + i % 4 < s.E;
+            z[i] = there ? v : 0.0f;
+            acc[i] += z[i];
+            amax = fmaxf(amax, fabsf(z[i]));
         }
+        if (a.dz && t < c1)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int e = e0 + 4 * s.G * v;
+                float* o = a.dz + (size_t)t * s.E + e;
+                if (s.vec4) {
+                    if (e < s.E) *reinterpret_cast<float4*>(o) = make_float4(z[4 * v], z[4 * v + 1], z[4 * v + 2], z[4 * v + 3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (e + i < s.E) o[i] = z[4 * v + i];
+                }
+            }
+        if (a.dz16) {
+            float up, down;
+            for (int o = s.G >> 1; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+            bal_scale(amax, up, down);
+            if (t < c1) {
+#pragma unroll
+                for (int v = 0; v < NV; ++v) {
+                    const int e = e0 + 4 * s.G * v;
+                    if (e < a.Ep) *reinterpret_cast<uint2*>(a.dz16 + (size_t)t * a.Ep + e) = bal_half4(z + 4 * v, up);
+                }
+                if (in_group == 0) a.row_scale[t] = down;
+            }
+        }
+        if (a.pieces && t < c1)
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                const int e = e0 + 4 * s.G * v;
+                if (e >= a.Ep) continue;
+#pragma unroll
+                for (int piece = 0; piece < 3; ++piece) {
+                    const uint2 r = make_uint2(pack_bf16x2(z[4 * v], z[4 * v + 1]), pack_bf16x2(z[4 * v + 2], z[4 * v + 3]));
+                    *reinterpret_cast<uint2*>(a.pieces + ((size_t)piece * s.T + t) * a.Ep + e) = r;
+                    z[4 * v] -= bf16_lo(r.x); z[4 * v + 1] -= bf16_hi(r.x); z[4 * v + 2] -= bf16_lo(r.y); z[4 * v + 3] -= bf16_hi(r.y);
+                }
+            }
     }
     if (!a.dbias_part) return;
     for (int o = s.G; o < 32; o <<= 1)
@@ -304,6 +413,269 @@ __global__ void __launch_bounds__(NV == 8 ? 256 : 512) balance_dz_kernel(const B
         a.dbias_part[(size_t)blockIdx.x * s.E + e] = v;
     }
 }
+
+// dW_r on CTA pairs: 256 rows of dW_r x up to 256 experts, K = the tokens.  As in route_score_pair_kernel, what bounds such a product
+// of three pieces is the traffic into shared memory, so a 64-token block of x (both operands lie with their columns contiguous) is
+// fetched once and multiplied with that block of all three pieces; x and the pieces travel through separate rings; and the K loop
+// is added up in segments of BW_SEG blocks, because the tensor core truncates where it adds.  The tokens are cut into `splits` ranges,
+// separate units of work whose sums balance_dw_sum_kernel adds in order.
+constexpr int BW_SA = 3, BW_SB = 9, BW_SLOT = 16384, BW_SEG = 3, BW_EPI_WARPS = 8;
+constexpr int BW_THREADS = 64 + 32 * BW_EPI_WARPS;
+constexpr int BW_SMEM_BYTES = (BW_SA + BW_SB) * BW_SLOT + 1024 /*align*/ + TC_BAR_BYTES;
+struct BalDwArgs {
+    BalSeqs q;
+    int T, d, E, splits;
+    float* out;            // splits == 1: dW_r; else the sums of the ranges, [splits][d][E]
+    int accumulate;        // splits == 1: add to dW_r
+    int x_split;           // d is no multiple of 64: one copy per 64-wide chunk of x, whose edge is zero-filled
+    int32_t* status;
+};
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BW_THREADS, 1)
+bal_dw_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constant__ CUtensorMap tmXe, const __grid_constant__ CUtensorMap tmP2,
+                   const __grid_constant__ CUtensorMap tmP1, const BalDwArgs args) {
+    extern __shared__ uint8_t tc_smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tc_smem_raw) + 1023) & ~uintptr_t(1023));
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (BW_SA + BW_SB) * BW_SLOT);
+    // bars: fullA[SA] (leader's are used), emptyA[SA] (both), fullB[SB] (leader's), emptyB[SB] (both),
+    //       tmem_full[2] (both), tmem_empty[2] (leader's)
+    constexpr int NBARS = 2 * BW_SA + 2 * BW_SB + 4;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + NBARS);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+    const int warp = warp_index(), lane = threadIdx.x % 32;
+    const uint32_t rank = cluster_ctarank();
+    const bool leader = rank == 0;
+    const uint32_t smem_base = smem_u32(smem);
+    const uint32_t bar_base = smem_u32(bars);
+    auto fullA = [&](int s) { return bar_base + 8u * s; };
+    auto emptyA = [&](int s) { return bar_base + 8u * (BW_SA + s); };
+    auto fullB = [&](int s) { return bar_base + 8u * (2 * BW_SA + s); };
+    auto emptyB = [&](int s) { return bar_base + 8u * (2 * BW_SA + BW_SB + s); };
+    auto tfull_bar = [&](int b) { return bar_base + 8u * (2 * BW_SA + 2 * BW_SB + b); };
+    auto tempty_bar = [&](int b) { return bar_base + 8u * (2 * BW_SA + 2 * BW_SB + 2 + b); };
+    auto slotA = [&](int s) { return smem_base + (uint32_t)s * BW_SLOT; };
+    auto slotB = [&](int s) { return smem_base + (uint32_t)(BW_SA + s) * BW_SLOT; };
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < 2 * BW_SA + 2 * BW_SB; ++s) mbar_init(bar_base + 8u * s, 1);
+        for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * BW_EPI_WARPS); }
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        tma_prefetch_desc(&tmX); tma_prefetch_desc(&tmXe); tma_prefetch_desc(&tmP2); tma_prefetch_desc(&tmP1);
+    }
+    if (warp == 1) tmem2_alloc(smem_u32(tmem_slot), 512);
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();          // the peer's barriers exist before anything signals them
+    tc_fence_after();
+    const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
+    pdl_begin();
+
+    const int begin = bal_off(args.q, 0), end = bal_off(args.q, args.q.S);
+    const int kb_first = begin / TC_BK, kblocks = end > begin ? (end - 1) / TC_BK + 1 - kb_first : 0;
+    const int tiles_n = (args.E + 255) / 256, tiles_m = (args.d + 255) / 256;
+    const int total = tiles_m * tiles_n * args.splits;
+    const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+    // columns of n-tile nt: 256, or 128 for a last tile of at most 128 columns
+    auto tile_cols = [&](int nt) { return (args.E - 256 * nt <= 128) ? 128 : 256; };
+    // unit of work -> rows of dW_r, experts, token blocks; the row tiles of one token range are neighbours and read the same pieces
+    struct Unit { int mt, nt, ks, kb0, kb1; };
+    auto decode = [&](int t) {
+        Unit u;
+        u.mt = t % tiles_m;
+        t /= tiles_m;
+        u.nt = t % tiles_n;
+        u.ks = t / tiles_n;
+        const int per = (kblocks + args.splits - 1) / args.splits;
+        u.kb0 = kb_first + min(kblocks, u.ks * per);
+        u.kb1 = kb_first + min(kblocks, (u.ks + 1) * per);
+        return u;
+    };
+
+    if (warp == 0) {
+        // ===================================================================== TMA producer (both CTAs)
+        const bool el = elect_one();
+        int sa = 0, sb = 0; uint32_t pa = 0, pb = 0; bool alive = true;
+        for (int t = cluster_id; t < total && alive; t += n_clusters) {
+            const Unit u = decode(t);
+            const int m0 = u.mt * 256 + 128 * (int)rank;          // past d: the copy fills zeros
+            const int half_cols = tile_cols(u.nt) >> 1;           // this CTA's columns: 64 or 128
+            const int chunk0 = (u.nt * 256 + (int)rank * half_cols) >> 6;
+            const CUtensorMap* mp = half_cols == 128 ? &tmP2 : &tmP1;
+            for (int kb = u.kb0; kb < u.kb1 && alive; ++kb) {
+                if (!mbar_wait_all(emptyA(sa), pa ^ 1u, abort_flag, args.status, STATUS_WAIT_EMPTY)) { alive = false; break; }
+                if (el) {
+                    if (leader) mbar_expect_tx(fullA(sa), 2 * BW_SLOT);
+                    const uint32_t fb = fullA(sa) & T2_PEER_MASK;
+                    const bool dirty = bal_dirty(kb, begin, end, args.T);
+                    const CUtensorMap* mx = dirty ? &tmXe : &tmX;
+                    const int k0 = !dirty ? kb * TC_BK : kb == kb_first ? 0 : TC_BK;
+                    if (!args.x_split) tma2_load_3d(slotA(sa), mx, fb, 0, k0, m0 >> 6);
+                    else {
+                        tma2_load_2d(slotA(sa), mx, fb, m0, k0);
+                        tma2_load_2d(slotA(sa) + TC_CHUNK_BYTES, mx, fb, m0 + 64, k0);
+                    }
+                }
+                if (++sa == BW_SA) { sa = 0; pa ^= 1u; }
+                for (int ph = 0; ph < 3; ++ph) {
+                    if (!mbar_wait_all(emptyB(sb), pb ^ 1u, abort_flag, args.status, STATUS_WAIT_EMPTY)) { alive = false; break; }
+                    if (el) {
+                        if (leader) mbar_expect_tx(fullB(sb), 2 * half_cols * TC_BK * 2);
+                        // chunked map {64 columns, T rows, Ep/64 chunks, 3 pieces}
+                        tma2_load_4d(slotB(sb), mp, fullB(sb) & T2_PEER_MASK, 0, kb * TC_BK, chunk0, ph);
+                    }
+                    if (++sb == BW_SB) { sb = 0; pb ^= 1u; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ===================================================================== MMA issuer (leader CTA)
+        if (leader) {
+            const bool el = elect_one();
+            // kind::f16, bf16 x bf16 -> fp32, both operands with their columns contiguous, M = 256 over the pair; N per tile
+            constexpr uint32_t idesc0 = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(256 >> 4) << 24);
+            const uint64_t desc = smem_desc(0, TC_CHUNK_BYTES, 1024);
+            constexpr uint32_t step = 2048 >> 4;        // 16 rows of K, 128 bytes each
+            int sa = 0, sb = 0; uint32_t pa = 0, pb = 0; int it = 0; bool alive = true;
+            for (int t = cluster_id; t < total && alive; t += n_clusters) {
+                const Unit u = decode(t);
+                if (u.kb0 >= u.kb1) continue;
+                const uint32_t idesc = idesc0 | ((uint32_t)(tile_cols(u.nt) >> 3) << 17);
+                uint32_t d_tmem = 0;
+                int kseg = BW_SEG;                       // K block inside the segment
+                for (int kb = u.kb0; kb < u.kb1 && alive; ++kb) {
+                    if (kseg == BW_SEG) {                // a new segment, in the other accumulator; the finished one goes to the epilogue
+                        if (kb > u.kb0) {
+                            if (el) umma2_commit_both(tfull_bar(it & 1));
+                            ++it;
+                        }
+                        kseg = 0;
+                        if (!mbar_wait_all(tempty_bar(it & 1), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, args.status,
+                                           STATUS_WAIT_TMEM_EMPTY)) { alive = false; break; }
+                        tc_fence_after();
+                        d_tmem = tmem_base + (uint32_t)(it & 1) * TC_BN;
+                    }
+                    if (!mbar_wait_all(fullA(sa), pa, abort_flag, args.status, STATUS_WAIT_FULL)) { alive = false; break; }
+                    const uint64_t da = desc | (uint64_t)((slotA(sa) & 0x3ffffu) >> 4);
+                    for (int ph = 0; ph < 3; ++ph) {
+                        if (!mbar_wait_all(fullB(sb), pb, abort_flag, args.status, STATUS_WAIT_FULL)) { alive = false; break; }
+                        tc_fence_after();
+                        const uint64_t db = desc | (uint64_t)((slotB(sb) & 0x3ffffu) >> 4);
+                        if (el) {
+#pragma unroll
+                            for (int k4 = 0; k4 < TC_BK / 16; ++k4)
+                                umma2_bf16(d_tmem, da + k4 * step, db + k4 * step, idesc, (kseg | ph | k4) != 0 ? 1u : 0u);
+                            umma2_commit_both(emptyB(sb));
+                        }
+                        if (++sb == BW_SB) { sb = 0; pb ^= 1u; }
+                    }
+                    if (!alive) break;
+                    if (el) umma2_commit_both(emptyA(sa));
+                    if (++sa == BW_SA) { sa = 0; pa ^= 1u; }
+                    ++kseg;
+                }
+                if (!alive) break;
+                if (el) umma2_commit_both(tfull_bar(it & 1));
+                ++it;
+            }
+        }
+    } else {
+        // ===================================================================== epilogue (8 warps, both CTAs)
+        const int quarter = warp & 3;            // TMEM lanes 32*quarter .. +31 belong to this warp
+        const int half = (warp - 2) >> 2;        // columns [128*half, 128*half + 128) of the tile
+        int it = 0;
+        bool ok = true;
+        for (int t = cluster_id; t < total && ok; t += n_clusters) {
+            const Unit u = decode(t);
+            const int nseg = (u.kb1 - u.kb0 + BW_SEG - 1) / BW_SEG;
+            const bool active = half * 128 < tile_cols(u.nt);
+            float sum[4][32];
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) sum[g][i] = 0.0f;
+            for (int sg = 0; sg < nseg; ++sg) {
+                const int b = it & 1;
+                if (!mbar_wait_warp(tfull_bar(b), (uint32_t)(it >> 1) & 1u, abort_flag, args.status, STATUS_WAIT_TMEM_FULL,
+                                    lane)) { ok = false; break; }
+                tc_fence_after();
+                if (active) {
+                    const uint32_t ta = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)b * TC_BN + half * 128;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        float part[32];
+                        tmem_ld32(ta + 32 * g, part);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sum[g][i] += part[i];
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(tempty_bar(b) & T2_PEER_MASK);
+                ++it;
+            }
+            if (!ok) break;
+            const int row = u.mt * 256 + 128 * (int)rank + quarter * 32 + lane;
+            if (active && row < args.d) {
+                float* out = args.out + ((size_t)u.ks * args.d + row) * args.E;
+                const bool add = args.accumulate && args.splits == 1;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const int col = u.nt * 256 + half * 128 + 32 * g;
+                    if (args.E % 4 == 0) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            if (col + i >= args.E) continue;
+                            float4 v = make_float4(sum[g][i], sum[g][i + 1], sum[g][i + 2], sum[g][i + 3]);
+                            if (add) {
+                                const float4 o = *reinterpret_cast<const float4*>(out + col + i);
+                                v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+                            }
+                            *reinterpret_cast<float4*>(out + col + i) = v;
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (col + i < args.E) out[col + i] = add ? out[col + i] + sum[g][i] : sum[g][i];
+                    }
+                }
+            }
+        }
+    }
+
+    // ------------------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < 2000000ll) __nanosleep(1000);
+        __syncthreads();
+    }
+    cluster_sync_all();          // neither CTA leaves while the other may still signal its barriers
+    if (warp == 1) {
+        tc_fence_after();
+        tmem2_dealloc(tmem_base, 512);
+    }
+}
+
+// The ranges' sums, added in order.
+__global__ void __launch_bounds__(256) balance_dw_sum_kernel(const float* __restrict__ part, float* __restrict__ dW, size_t n, int splits,
+                                                             int accumulate) {
+    pdl_begin();
+    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; 4 * i < n; i += (size_t)gridDim.x * blockDim.x) {
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        float4* o = reinterpret_cast<float4*>(dW) + i;       // (n = d E is a multiple of 4: d is one of 8)
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s) {
+            const float4 p = reinterpret_cast<const float4*>(part + s * n)[i];
+            v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+        }
+        if (accumulate) { v.x += o->x; v.y += o->y; v.z += o->z; v.w += o->w; }
+        *o = v;
+    }
+}
+
 __global__ void __launch_bounds__(256) balance_dbias_kernel(const float* __restrict__ part, float* __restrict__ dbias, int blocks, int E,
                                                             int accumulate) {
     pdl_begin();
@@ -314,6 +686,7 @@ __global__ void __launch_bounds__(256) balance_dbias_kernel(const float* __restr
     dbias[e] = accumulate ? dbias[e] + v : v;
 }
 
+// The same products on the CUDA cores, for contexts whose GEMMs run there (MOP_GEMM_SCALAR).
 // dW_r = x^T dz over the tokens of the sequences; 64 x 64 outputs a block, 4 x 4 a thread.
 __global__ void __launch_bounds__(256) balance_dw_kernel(const bf16* __restrict__ x, const float* __restrict__ dz, const BalSeqs q,
                                                          float* __restrict__ dW, int d, int E, int accumulate) {
@@ -385,6 +758,8 @@ __global__ void __launch_bounds__(256) balance_dx_kernel(const float* __restrict
 }
 
 // ------------------------------------------------------------------------------------------ host
+constexpr int BAL_MAX_SPLITS = 16;
+constexpr int BAL_PAIRS = 74;             // CTA pairs that the rules below count with (148 SMs)
 // Tokens per block: one block for each SM, at least 16 tokens each.
 inline int bal_chunk(int T) { const int c = (T + 147) / 148; return c < 16 ? 16 : c; }
 inline int bal_blocks(int T) { return (T + bal_chunk(T) - 1) / bal_chunk(T); }
@@ -392,6 +767,26 @@ inline int bal_warps(int E) { return E <= 512 ? 16 : 8; }
 inline size_t bal_smem_bytes(int E, int warps) { return (size_t)(warps + 1) * E * 4; }
 inline BalShape bal_shape(const mop_moe_shape& s) {
     return {s.T, s.E, s.k, bal_group(s.E), s.score_fn, s.E % 4 == 0};
+}
+// Lanes per token in the backward: whole 64-wide blocks of experts, for the zeros behind the last one.
+inline int bal_group_bwd(int E) { return E <= 64 ? 16 : 32; }
+inline mop_status bal_init() {
+    if (cudaFuncSetAttribute(bal_dw_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BW_SMEM_BYTES) != cudaSuccess) return MOP_ERR_CUDA;
+    return vd_set_smem<VD_R>();
+}
+// Token ranges of the dW_r product: the makespan of the round-robin over the pairs, in microseconds.  A token block of a tile takes 0.8
+// (256 experts) or 0.4, a unit 2.5 more to fill its rings and store its tile, and a further range costs its sums' way to L2 and back.
+inline int bal_splits(int T, int d, int E, int pairs) {
+    const int tiles = ((d + 255) / 256) * ((E + 255) / 256), kb = (T + 63) / 64;
+    const double t_kb = E <= 128 ? 0.4 : 0.8, t_sum = 8e-6 * d * E / 5.0;
+    int pick = 1;
+    double best = 1e30;
+    for (int s = 1; s <= BAL_MAX_SPLITS && s <= kb; ++s) {
+        const int rounds = (tiles * s + pairs - 1) / pairs;
+        const double t = rounds * (((kb + s - 1) / s) * t_kb + 2.5) + (s > 1 ? 3.0 + t_sum * s : 0.0);
+        if (t < best) { best = t; pick = s; }
+    }
+    return pick;
 }
 #define BAL_BY_WIDTH(E, GO)                                       \
     do {                                                          \

@@ -9,7 +9,8 @@
 //   VD_L  Y = X W_voc: per row and 128 columns the maximum and the sum of exponentials, and the logits of the teacher's entries
 //   VD_P  dY, one block of vocabulary columns, bf16 (the only piece of the N x V matrix that ever exists)
 //   VD_W  dW_voc[:, block] = X^T dY, bf16
-// and dX += dY W_voc^T runs on tc_gemm2_kernel<TC_VX>, beside VD_W.
+// and dX += dY W_voc^T runs on tc_gemm2_kernel<TC_VX>, beside VD_W.  A fourth one is the router's (balance.cuh):
+//   VD_R  dX (+)= dz W_r^T from fp16 operands whose rows are scaled by powers of two, bf16
 //
 // A row's entries are sorted by column first (distill_prep_kernel), so that the thread that owns the row finds those of its 128
 // columns by one binary search while the tile is being multiplied.
@@ -20,7 +21,7 @@
 
 namespace mop {
 
-enum : int { VD_L = 0, VD_P = 1, VD_W = 2 };
+enum : int { VD_L = 0, VD_P = 1, VD_W = 2, VD_R = 3 };
 
 constexpr int VD_STAGES = 6;
 constexpr int VD_EPI_WARPS = 8;
@@ -46,6 +47,10 @@ struct VdArgs {
     float2* part;                 // VD_L: [2 tiles_n][N] (maximum, sum)
     const float* coef;            // VD_P: dloss / tau Q per row
     const float* lse2;            // VD_P: log-sum-exp per row in units of log 2
+    const float *row_scale, *col_scale;   // VD_R: what undoes the operands' scaling, per token and per column of dX
+    bf16* add_to;                 // VD_R: dX [N, cols] that the product is added to, or null
+    const int32_t* seq_off;       // VD_R: offsets of the sequences or null: rows outside [seq_off[0], seq_off[n_seq]) keep what they hold
+    int n_seq;
     int32_t* status;
     bool gemm_follows;
     PdlNote note;
@@ -73,6 +78,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                const VdArgs args) {
     constexpr int S = VD_STAGES;
     constexpr bool A_MN = KIND == VD_W;                       // the tokens are K: X^T lies with M contiguous
+    constexpr bool B_MN = KIND != VD_R;
     extern __shared__ uint8_t tc_smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tc_smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* boxes = smem + S * T2_STAGE_BYTES;
@@ -138,7 +144,8 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                         tma2_load_2d(sA, &tmA, fb, m0, k0);
                         tma2_load_2d(sA + TC_CHUNK_BYTES, &tmA, fb, m0 + 64, k0);
                     }
-                    if (!args.b_split) tma2_load_3d(sB, &tmB, fb, 0, k0, n0 >> 6);
+                    if constexpr (!B_MN) tma2_load_2d(sB, &tmB, fb, k0, n0);
+                    else if (!args.b_split) tma2_load_3d(sB, &tmB, fb, 0, k0, n0 >> 6);
                     else {
                         tma2_load_2d(sB, &tmB, fb, n0, k0);
                         tma2_load_2d(sB + TC_CHUNK_BYTES, &tmB, fb, n0 + 64, k0);
@@ -151,10 +158,11 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         // ===================================================================== MMA issuer (leader CTA)
         if (leader) {
             const bool el = elect_one();
-            constexpr uint32_t idesc = make_idesc2(A_MN, true);
+            // VD_R: both operands fp16 (format 0) instead of bf16 (1)
+            constexpr uint32_t idesc = make_idesc2(A_MN, B_MN) & (KIND == VD_R ? ~((1u << 7) | (1u << 10)) : ~0u);
             const uint64_t desc_a = A_MN ? smem_desc(0, TC_CHUNK_BYTES, 1024) : smem_desc(0, 0, 1024);
-            const uint64_t desc_b = smem_desc(0, TC_CHUNK_BYTES, 1024);
-            constexpr uint32_t a_step = (A_MN ? 2048 : 32) >> 4, b_step = 2048 >> 4;
+            const uint64_t desc_b = B_MN ? smem_desc(0, TC_CHUNK_BYTES, 1024) : smem_desc(0, 0, 1024);
+            constexpr uint32_t a_step = (A_MN ? 2048 : 32) >> 4, b_step = (B_MN ? 2048 : 32) >> 4;
             int stage = 0; uint32_t phase = 0; int it = 0; bool alive = true;
             for (int t = cluster_id; t < total && alive; t += n_clusters) {
                 uint32_t d_tmem = 0;
@@ -261,6 +269,11 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             } else {
                 const bool mine = row < args.N;
                 float coef = 0.0f, lse2 = 0.0f;
+                bool inside = true;
+                if constexpr (KIND == VD_R) {
+                    if (mine) coef = args.row_scale[row];
+                    if (args.add_to && args.seq_off) inside = row >= __ldg(args.seq_off) && row < __ldg(args.seq_off + args.n_seq);
+                }
                 int at = args.K, next = INT_MAX;
                 const int32_t* list = args.scol + (size_t)row * args.K;
                 if constexpr (KIND == VD_P) {
@@ -276,6 +289,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 if (!bar_vote_all(1 + half, 128, ready)) { ok = false; break; }
                 tc_fence_after();
                 float y[4][32];
+                (void)inside;
                 const uint32_t ta = ta0 + (uint32_t)(it & 1) * TC_BN;
                 tmem_ld32_nowait(ta, y[0]);
                 tmem_ld32_nowait(ta + 32, y[1]);
@@ -296,13 +310,37 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                         for (int g = 2 * h; g < 2 * h + 2; ++g)
 #pragma unroll
                             for (int i = 0; i < 32; ++i) y[g][i] = coef * ex2(fmaf(y[g][i], args.c, -lse2));
+                    if constexpr (KIND == VD_R) {
+#pragma unroll
+                        for (int g = 2 * h; g < 2 * h + 2; ++g)
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4) {
+                                const float4 s = __ldg(reinterpret_cast<const float4*>(args.col_scale + col0 + 32 * g + i));
+                                y[g][i] = y[g][i] * s.x * coef;
+                                y[g][i + 1] = y[g][i + 1] * s.y * coef;
+                                y[g][i + 2] = y[g][i + 2] * s.z * coef;
+                                y[g][i + 3] = y[g][i + 3] * s.w * coef;
+                            }
+                    }
                     if (issuer) tma_store_wait_read<0>(); // the box's last copy has been read
                     asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        const float* v = &y[2 * h + j / 4][(j % 4) * 8];
-                        *reinterpret_cast<uint4*>(rowp + ((j ^ (lane & 7)) << 4)) =
-                            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+                        float* v = &y[2 * h + j / 4][(j % 4) * 8];
+                        uint4 o;
+                        if constexpr (KIND == VD_R) {
+                            const int col = col0 + 64 * h + 8 * j;
+                            if (args.add_to && mine && col < args.cols) {
+                                o = *reinterpret_cast<const uint4*>(args.add_to + (size_t)row * args.cols + col);
+                                if (inside) {
+                                    v[0] += bf16_lo(o.x); v[1] += bf16_hi(o.x); v[2] += bf16_lo(o.y); v[3] += bf16_hi(o.y);
+                                    v[4] += bf16_lo(o.z); v[5] += bf16_hi(o.z); v[6] += bf16_lo(o.w); v[7] += bf16_hi(o.w);
+                                }
+                            }
+                        }
+                        if (KIND != VD_R || inside)
+                            o = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+                        *reinterpret_cast<uint4*>(rowp + ((j ^ (lane & 7)) << 4)) = o;
                     }
                     if constexpr (KIND == VD_P)
                         while (next < col0 + 64 * (h + 1)) {              // the teacher's entries among these columns
@@ -316,7 +354,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                     asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
                     if (issuer) {
                         const int x = 256 * nt + 128 * half + 64 * h, r0 = 256 * mt + 128 * (int)rank;
-                        if (x < args.cols && r0 < (KIND == VD_P ? args.N : args.H)) tma_store_2d(&tmO, smem_u32(box), x, r0);
+                        if (x < args.cols && r0 < (KIND == VD_W ? args.H : args.N)) tma_store_2d(&tmO, smem_u32(box), x, r0);
                         tma_store_commit();
                     }
                 }
@@ -547,6 +585,7 @@ inline mop_status vd_init() {
     mop_status r;
     if ((r = vd_set_smem<VD_L>()) != MOP_OK) return r;
     if ((r = vd_set_smem<VD_P>()) != MOP_OK) return r;
+    if ((r = vd_set_smem<VD_R>()) != MOP_OK) return r;
     return vd_set_smem<VD_W>();
 }
 template <int KIND>

@@ -14,8 +14,8 @@
 #include "gemm_host.cuh"
 #include "gemm_rs.cuh"
 #include "route_permute.cuh"
-#include "balance.cuh"
 #include "distill.cuh"
+#include "balance.cuh"
 
 using namespace mop;
 
@@ -416,6 +416,7 @@ mop_status mop_create(mop_ctx** out, const mop_moe_shape* shape, int device) {
         if (st == MOP_OK) st = tn_init();
         if (st == MOP_OK) st = tw_init();
         if (st == MOP_OK) st = rs_init();
+        if (st == MOP_OK) st = bal_init();
         if (st != MOP_OK) { cudaFree(c->ws); delete c; return st; }
         if (c->fast_route) {
             bool ok = cudaMemset(c->fr_scal, 0, 256) == cudaSuccess;
@@ -1157,18 +1158,29 @@ mop_status mop_moe_route_bwd(mop_ctx* c, const float* logits, const float* bias,
 // Load-balance loss of the router and its gradients (the caller owns the workspace)
 // ---------------------------------------------------------------------------------------------
 namespace {
-struct BalanceLayout { size_t part_p, part_c, dz, dbias, total; };
+struct BalanceLayout { size_t part_p, part_c, dz, dbias, pieces, dz16, row_scale, w16, col_scale, xe, dw_part, total; };
 BalanceLayout balance_layout(const mop_moe_shape& s, bool backward) {
     BalanceLayout L{};
     size_t o = 0;
     auto take = [&](size_t b) { size_t r = o; o += align_up(b); return r; };
-    const size_t blocks = bal_blocks(s.T), E = s.E;
+    const size_t blocks = bal_blocks(s.T), T = s.T, d = s.d, E = s.E, Ep = bal_ep(s.E);
     if (!backward) {
         L.part_p = take(2 * blocks * E * 4);
         L.part_c = take(2 * blocks * E * 4);
     } else {
-        L.dz = take((size_t)s.T * E * 4);
         L.dbias = take(blocks * E * 4);
+        if (s.gemm_path == MOP_GEMM_SCALAR) {
+            L.dz = take(T * E * 4);
+        } else {
+            L.pieces = take(3 * T * Ep * 2);
+            L.dz16 = take(T * Ep * 2);
+            L.row_scale = take(T * 4);
+            L.w16 = take(d * Ep * 2);
+            L.col_scale = take((d + 255) / 256 * 1024);
+            L.xe = take(128 * d * 2);
+            const int splits = bal_splits(s.T, s.d, s.E, BAL_PAIRS);
+            if (splits > 1) L.dw_part = take((size_t)splits * d * E * 4);
+        }
     }
     L.total = o;
     return L;
@@ -1245,29 +1257,76 @@ mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logi
     }
     const BalanceLayout L = balance_layout(s, true);
     char* w = static_cast<char*>(workspace);
+    const bool tensor = use_tensor(c);
     BalBwdArgs a{};
     a.logits = logits; a.bias = pre ? bias : nullptr; a.counts = counts; a.dloss = dloss;
-    a.q = {seq_offsets, n_seq, s.T}; a.s = bal_shape(s); a.chunk = bal_chunk(s.T);
-    a.dz = dlogits_opt ? dlogits_opt : reinterpret_cast<float*>(w + L.dz);
+    a.q = {seq_offsets, n_seq, s.T}; a.s = bal_shape(s); a.s.G = bal_group_bwd(s.E);
+    a.chunk = bal_chunk(s.T); a.dz_blocks = bal_blocks(s.T);
+    a.dz = dlogits_opt;
     a.dbias_part = pre && dbias_opt ? reinterpret_cast<float*>(w + L.dbias) : nullptr;
-    const int warps = bal_warps(s.E), blocks = bal_blocks(s.T);
-#define GO(NV) pdl_launch(balance_dz_kernel<NV>, blocks, 32 * warps, bal_smem_bytes(s.E, warps), st, a)
+    const int warps = bal_warps(s.E);
+    int extra = 0;
+    if (tensor) {
+        a.Ep = bal_ep(s.E); a.d = s.d;
+        if (dW_r_opt) {
+            a.pieces = reinterpret_cast<bf16*>(w + L.pieces);
+            a.x = static_cast<const uint4*>(x); a.xe = reinterpret_cast<uint4*>(w + L.xe);
+            extra += 2 * BAL_EDGE_BLOCKS;
+        }
+        if (dX_opt) {
+            a.dz16 = reinterpret_cast<__half*>(w + L.dz16); a.row_scale = reinterpret_cast<float*>(w + L.row_scale);
+            a.W_r = W_r; a.w16 = reinterpret_cast<__half*>(w + L.w16); a.col_scale = reinterpret_cast<float*>(w + L.col_scale);
+            extra += min(ceil_div(s.d, warps), 2 * c->sm_count);
+        }
+    } else if (!a.dz && (dW_r_opt || dX_opt)) a.dz = reinterpret_cast<float*>(w + L.dz);
+#define GO(NV) pdl_launch(balance_dz_kernel<NV>, a.dz_blocks + extra, 32 * warps, bal_smem_bytes(s.E, warps), st, a)
     LAUNCH(c, "balance_dz", st, BAL_BY_WIDTH(s.E, GO));
 #undef GO
     mop_status r = after_launch(c);
     if (r != MOP_OK) return r;
     if (a.dbias_part) {
         LAUNCH(c, "balance_dbias", st,
-               pdl_launch(balance_dbias_kernel, ceil_div(s.E, 256), 256, 0, st, a.dbias_part, dbias_opt, blocks, s.E, accumulate));
+               pdl_launch(balance_dbias_kernel, ceil_div(s.E, 256), 256, 0, st, a.dbias_part, dbias_opt, a.dz_blocks, s.E, accumulate));
         if ((r = after_launch(c)) != MOP_OK) return r;
     }
-    if (dW_r_opt) {
+    if (dW_r_opt && tensor) {
+        BalDwArgs g{};
+        g.q = a.q; g.T = s.T; g.d = s.d; g.E = s.E; g.splits = bal_splits(s.T, s.d, s.E, BAL_PAIRS);
+        g.out = g.splits > 1 ? reinterpret_cast<float*>(w + L.dw_part) : dW_r_opt;
+        g.accumulate = accumulate; g.x_split = s.d % 64 != 0; g.status = c->status;
+        CUtensorMap mX, mXe, mP2, mP1;
+        if (!tc_map_mn(&c->plan, &mX, x, s.T, s.d, 2) || !tc_map_mn(&c->plan, &mXe, a.xe, 128, s.d, 2) ||
+            !tc_map_chunked_3d(&c->plan, &mP2, a.pieces, 3, s.T, a.Ep, 2) || !tc_map_chunked_3d(&c->plan, &mP1, a.pieces, 3, s.T, a.Ep, 1))
+            return MOP_ERR_CUDA;
+        LAUNCH(c, "balance_dw", st,
+               pdl_launch(bal_dw_pair_kernel, c->sm_count & ~1, BW_THREADS, BW_SMEM_BYTES, st, mX, mXe, mP2, mP1, g));
+        if ((r = after_launch(c)) != MOP_OK) return r;
+        if (g.splits > 1) {
+            const size_t n = (size_t)s.d * s.E;
+            LAUNCH(c, "balance_dw_sum", st,
+                   pdl_launch(balance_dw_sum_kernel, (unsigned)min((n / 4 + 255) / 256, (size_t)c->sm_count * 8), 256, 0, st, g.out,
+                              dW_r_opt, n, g.splits, accumulate));
+            if ((r = after_launch(c)) != MOP_OK) return r;
+        }
+    } else if (dW_r_opt) {
         LAUNCH(c, "balance_dw", st,
                pdl_launch(balance_dw_kernel, dim3(ceil_div(s.d, 64), ceil_div(s.E, 64)), 256, 0, st, static_cast<const bf16*>(x), a.dz,
                           a.q, dW_r_opt, s.d, s.E, accumulate));
         if ((r = after_launch(c)) != MOP_OK) return r;
     }
-    if (dX_opt) {
+    if (dX_opt && tensor) {
+        VdArgs g{};
+        g.N = s.T; g.H = s.d; g.tiles_m = ceil_div(s.T, 256); g.tiles_n = ceil_div(s.d, 256); g.n_group = g.tiles_n;
+        g.kblocks = a.Ep / TC_BK; g.cols = s.d; g.row_scale = a.row_scale; g.col_scale = a.col_scale;
+        g.add_to = accumulate ? static_cast<bf16*>(dX_opt) : nullptr; g.seq_off = seq_offsets; g.n_seq = n_seq;
+        g.status = c->status;
+        CUtensorMap mA, mB, mO;
+        if (!tc_map_2d(&c->plan, &mA, a.dz16, s.T, a.Ep, 128) || !tc_map_2d(&c->plan, &mB, a.w16, s.d, a.Ep, 128) ||
+            !vd_map_out(&c->plan, &mO, dX_opt, s.T, s.d, s.d))
+            return MOP_ERR_CUDA;
+        LAUNCH(c, "balance_dx", st, r = vd_launch<VD_R>(&c->plan, mA, mB, mO, g, st));
+        if (r == MOP_OK) r = after_launch(c);
+    } else if (dX_opt) {
         LAUNCH(c, "balance_dx", st,
                pdl_launch(balance_dx_kernel, dim3(ceil_div(s.d, 64), ceil_div(s.T, 64)), 256, 0, st, a.dz, W_r, a.q,
                           static_cast<bf16*>(dX_opt), s.T, s.d, s.E, accumulate));

@@ -22,7 +22,7 @@ P_RTOL = 1.3e-5
 class Case:
     """Inputs on the device (padding rows hold NaN everywhere), a context and a workspace that starts as NaN."""
 
-    def __init__(self, T, d, E, k, score, mode, off, seed=0, std=1.5):
+    def __init__(self, T, d, E, k, score, mode, off, seed=0, std=1.5, path=binding.GEMM_AUTO):
         g = torch.Generator(device="cuda").manual_seed(seed + 17)
         self.T, self.d, self.E, self.k, self.score, self.mode, self.off = T, d, E, k, score, mode, off
         self.logits = torch.randn((T, E), generator=g, device="cuda") * std
@@ -41,7 +41,7 @@ class Case:
         self.logits[self.pad] = float("nan")
         self.x[self.pad] = float("nan")
         self.idx[self.pad] = 1 << 30
-        self.ctx = binding.Context(T, d, E, k, 64, score, mode)
+        self.ctx = binding.Context(T, d, E, k, 64, score, mode, gemm_path=path)
 
     def workspace(self, backward):
         n = max(256, binding.mop_moe_balance_workspace_bytes(self.ctx, self.S, backward))
@@ -152,6 +152,32 @@ def test_balance_loss_and_gradients_match_the_oracle(T, d, E, k, score, mode, of
         check_backward(c, out, 0.5, accumulate)
         again = c.backward(got[0], c.outputs(0.5), accumulate)
         assert all(torch.equal(out[n], again[n]) for n in out)
+    binding.mop_poll(c.ctx)
+
+
+@pytest.mark.parametrize("T,d,E,k,score,mode,off", [(37, 72, 5, 3, SOFTMAX, PRE, [0, 1, 1, 30, 37]), (300, 200, 130, 3, SIGMOID, PRE, [11, 60, 60, 61, 290])],
+                         ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_the_products_on_the_cuda_cores(T, d, E, k, score, mode, off):
+    c = Case(T, d, E, k, score, mode, off, seed=T, path=binding.GEMM_SCALAR)
+    got = c.forward()
+    check_forward(c, got)
+    for accumulate in (False, True):
+        check_backward(c, c.backward(got[0], c.outputs(0.5), accumulate), 0.5, accumulate)
+    out = {"dW_r": c.outputs()["dW_r"]}                                   # (dz in the workspace)
+    check_backward(c, c.backward(got[0], out))
+
+
+@pytest.mark.parametrize("T,d,E,off", [(4100, 328, 72, [70, 4000]),       # ranges of tokens; both edge blocks hold padding; E in one narrow tile
+                                       (64 * 40, 512, 300, [64, 64 * 39]),  # edges on block borders; a wide and a narrow tile
+                                       (1000, 2064, 256, [130, 150]),      # all tokens inside one block
+                                       (5000, 264, 200, [0, 4999])],       # one token of padding
+                         ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_ranges_of_tokens_that_fit_no_block(T, d, E, off):
+    c = Case(T, d, E, 4, SOFTMAX, NONE, off, seed=d)
+    got = c.forward()
+    check_forward(c, got)
+    check_backward(c, c.backward(got[0], c.outputs()))
+    check_backward(c, c.backward(got[0], c.outputs(0.5), True), 0.5, True)
     binding.mop_poll(c.ctx)
 
 
