@@ -4,16 +4,16 @@
 //   loss[n] = sum_k q_k (log q_k - s[n, i_k] + lse[n])
 //   dY[n,v] = dloss[n] / tau (Q p[n,v] - sum_{k: i_k = v} q_k),   p = exp(s - lse),   Q = sum_k q_k
 //
-// vd_gemm_kernel runs three products on CTA pairs (256 x 256 tiles, tcgen05.mma.cta_group::2, six stages of 64 of K, as
+// vd_gemm_kernel runs the products on CTA pairs (256 x 256 tiles, tcgen05.mma.cta_group::2, stages of 64 of K, as
 // tc_gemm2_kernel), with eight epilogue warps:
 //   VD_L  Y = X W_voc: per row and 128 columns the maximum and the sum of exponentials, and the logits of the teacher's entries
 //   VD_P  dY, one block of vocabulary columns, bf16 (the only piece of the N x V matrix that ever exists)
 //   VD_W  dW_voc[:, block] = X^T dY, bf16
-// and dX += dY W_voc^T runs on tc_gemm2_kernel<TC_VX>, beside VD_W.  A fourth one is the router's (balance.cuh):
-//   VD_R  dX (+)= dz W_r^T from fp16 operands whose rows are scaled by powers of two, bf16
+//   VD_X  dX = dY W_voc^T, beside VD_W: the block's columns (its K) in `splits` ranges, fp32 sums over the blocks
+//   VD_R  the router's dX (+)= dz W_r^T (balance.cuh) from fp16 operands whose rows are scaled by powers of two, bf16
 //
-// A row's entries are sorted by column first (distill_prep_kernel), so that the thread that owns the row finds those of its 128
-// columns by one binary search while the tile is being multiplied.
+// A row's entries are sorted by column first (distill_prep_kernel), with the number of entries below each 128 columns beside
+// them: the thread that owns the row fetches those of its columns while the tile is being multiplied.
 #pragma once
 #include <limits.h>
 
@@ -21,13 +21,19 @@
 
 namespace mop {
 
-enum : int { VD_L = 0, VD_P = 1, VD_W = 2, VD_R = 3 };
+enum : int { VD_L = 0, VD_P = 1, VD_W = 2, VD_R = 3, VD_X = 4 };
 
-constexpr int VD_STAGES = 6;
+// Stages, and store boxes (128 rows x 64 bf16 columns) for each column half: one is read by the copy engine while the next is filled.
+template <int KIND>
+struct VdTraits {
+    static constexpr bool STORES = KIND != VD_L;
+    static constexpr int BOXES = STORES ? 2 : 0;
+    static constexpr int STAGES = STORES ? 5 : 6;
+    static constexpr int SMEM_BYTES = STAGES * T2_STAGE_BYTES + 2 * BOXES * 16384 + 1024 /*align*/ + TC_BAR_BYTES;
+};
 constexpr int VD_EPI_WARPS = 8;
 constexpr int VD_THREADS = 64 + 32 * VD_EPI_WARPS;
-constexpr int VD_BOX_BYTES = 128 * 64 * 2;                    // store box: 128 rows x 64 bf16 columns, one for each column half
-constexpr int VD_SMEM_BYTES = VD_STAGES * T2_STAGE_BYTES + 2 * VD_BOX_BYTES + 1024 /*align*/ + TC_BAR_BYTES;
+constexpr int VD_BOX_BYTES = 128 * 64 * 2;
 // K blocks (of 64) per accumulation segment of the forward.  The tensor core truncates where it adds; a segment starts from zero and
 // the finished ones are added in fp32 registers, rounding to nearest.
 constexpr int VD_SEG = 4;
@@ -37,20 +43,24 @@ struct VdArgs {
     int N, H, V, K;               // tokens, hidden size, vocabulary, entries per token
     int tiles_m, tiles_n, n_group, kblocks;
     int n_base;                   // VD_P: first vocabulary column of the block
-    int cols;                     // VD_L, VD_P: columns of the whole matrix that exist (V)
+    int k_base;                   // VD_X: the same, added to W's K coordinate
+    int cols;                     // columns of the whole output that exist
     int a_split, b_split;         // that operand's columns are no multiple of 64: one copy per 64-wide chunk, whose edge is zero-filled
+    int splits;                   // VD_X: ranges of K, as separate units of work (1 elsewhere)
     float c;                      // log2(e) / tau
-    const int32_t* scol;          // [N, K] columns of the entries, ascending (INT_MAX: none)
-    const int32_t* sslot;         // VD_L: the place of each in the caller's list
-    const float* sval;            // VD_P: dY of each
+    const int2* entry;            // [N, K] the row's entries by column (ascending): {column, place in the caller's list (VD_L) or dY (VD_P)}
+    const uint16_t* first;        // [N, units + 1] how many of them lie below column 128 u
+    int units;
     float* student;               // VD_L: [N, K] logits at the entries
-    float2* part;                 // VD_L: [2 tiles_n][N] (maximum, sum)
+    float2* part;                 // VD_L: [N, units] (maximum, sum)
     const float* coef;            // VD_P: dloss / tau Q per row
     const float* lse2;            // VD_P: log-sum-exp per row in units of log 2
     const float *row_scale, *col_scale;   // VD_R: what undoes the operands' scaling, per token and per column of dX
     bf16* add_to;                 // VD_R: dX [N, cols] that the product is added to, or null
     const int32_t* seq_off;       // VD_R: offsets of the sequences or null: rows outside [seq_off[0], seq_off[n_seq]) keep what they hold
     int n_seq;
+    float* dx32;                  // VD_X: [splits, N, pitch] fp32 sums, or null: one range and one block, dX is stored at once
+    int pitch, accumulate;        // VD_X: add to them
     int32_t* status;
     bool gemm_follows;
     PdlNote note;
@@ -62,27 +72,46 @@ __device__ __forceinline__ float ex2(float v) {
     return r;
 }
 
-// First of the row's sorted columns that is not below `col`.
-__device__ __forceinline__ int vd_first(const int32_t* __restrict__ row, int K, int col) {
-    int lo = 0, hi = K;
-    while (lo < hi) {
-        const int mid = (lo + hi) >> 1;
-        if (__ldg(row + mid) < col) lo = mid + 1; else hi = mid;
+// The entries of a row among 128 columns, in ascending order: the next four are in registers.
+struct VdEntries {
+    const int2* list;
+    int left;                     // entries that are not in registers yet
+    int2 e[4];
+    __device__ __forceinline__ void open(const VdArgs& a, int row, int unit, bool on) {
+        left = 0;
+        list = a.entry;
+        if (on) {
+            const uint16_t* f = a.first + (size_t)row * (a.units + 1) + unit;
+            const int from = __ldg(f);
+            left = (int)__ldg(f + 1) - from;
+            list = a.entry + (size_t)row * a.K + from;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { e[i] = make_int2(INT_MAX, 0); if (i < left) e[i] = __ldg(list + i); }
+        list += 4;
+        left -= 4;
     }
-    return lo;
-}
+    __device__ __forceinline__ int2 take() {
+        const int2 r = e[0];
+        e[0] = e[1]; e[1] = e[2]; e[2] = e[3];
+        e[3] = make_int2(INT_MAX, 0);
+        if (left > 0) { e[3] = __ldg(list); ++list; --left; }
+        return r;
+    }
+};
 
 template <int KIND>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VD_THREADS, 1)
 vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO,
                const VdArgs args) {
-    constexpr int S = VD_STAGES;
+    using Tr = VdTraits<KIND>;
+    constexpr int S = Tr::STAGES;
     constexpr bool A_MN = KIND == VD_W;                       // the tokens are K: X^T lies with M contiguous
-    constexpr bool B_MN = KIND != VD_R;
+    constexpr bool B_MN = KIND != VD_R && KIND != VD_X;
     extern __shared__ uint8_t tc_smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tc_smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* boxes = smem + S * T2_STAGE_BYTES;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(boxes + 2 * VD_BOX_BYTES);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(boxes + 2 * Tr::BOXES * VD_BOX_BYTES);
     // bars: [0,S) full (leader's are used), [S,2S) empty (both), tmem_full[2] (both), tmem_empty[2] (leader's)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * S + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -103,7 +132,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tma_prefetch_desc(&tmA); tma_prefetch_desc(&tmB);
-        if (KIND != VD_L) tma_prefetch_desc(&tmO);
+        if (Tr::STORES) tma_prefetch_desc(&tmO);
     }
     if (warp == 1) tmem2_alloc(smem_u32(tmem_slot), 512);
     tc_fence_before();
@@ -111,12 +140,21 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     cluster_sync_all();          // the peer's barriers exist before anything signals them
     tc_fence_after();
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-    pdl_begin_gemm(args.gemm_follows, args.note);
+    // dX runs beside the weight gradient of its block: both read the logit gradients, neither what the other writes.
+    if constexpr (KIND == VD_X) pdl_begin_beside(args.gemm_follows, args.note);
+    else pdl_begin_gemm(args.gemm_follows, args.note);
 
-    const int total = args.tiles_m * args.tiles_n, nkb = args.kblocks;
+    const int tiles = args.tiles_m * args.tiles_n, total = KIND == VD_X ? tiles * args.splits : tiles;
     const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
     // blocks of n_group n-tiles, row tiles slower inside one: the pairs that run at the same time cover a nearly square patch
-    auto decode = [&](int t, int& mt, int& nt) {
+    auto decode = [&](int t, int& mt, int& nt, int& kb0, int& kb1) {
+        kb0 = 0; kb1 = args.kblocks;
+        if constexpr (KIND == VD_X) {
+            const int ks = t / tiles, q = args.kblocks / args.splits, r = args.kblocks - q * args.splits;
+            t -= ks * tiles;
+            kb0 = ks * q + min(ks, r);
+            kb1 = kb0 + q + (ks < r ? 1 : 0);
+        }
         const int per = args.n_group * args.tiles_m, g = t / per, r = t - g * per;
         const int w = min(args.n_group, args.tiles_n - g * args.n_group);
         mt = r / w;
@@ -128,10 +166,10 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const bool el = elect_one();
         int stage = 0; uint32_t phase = 0; bool alive = true;
         for (int t = cluster_id; t < total && alive; t += n_clusters) {
-            int mt, nt;
-            decode(t, mt, nt);
+            int mt, nt, kb0, kb1;
+            decode(t, mt, nt, kb0, kb1);
             const int m0 = 256 * mt + 128 * (int)rank, n0 = args.n_base + 256 * nt + 128 * (int)rank;
-            for (int kb = 0; kb < nkb; ++kb) {
+            for (int kb = kb0; kb < kb1; ++kb) {
                 if (!mbar_wait_all(empty_bar(stage), phase ^ 1u, abort_flag, args.status, STATUS_WAIT_EMPTY)) { alive = false; break; }
                 const uint32_t fb = full_bar(stage) & T2_PEER_MASK;    // the leader's barrier
                 const uint32_t sA = smem_base + stage * T2_STAGE_BYTES, sB = sA + T2_A_BYTES;
@@ -144,7 +182,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                         tma2_load_2d(sA, &tmA, fb, m0, k0);
                         tma2_load_2d(sA + TC_CHUNK_BYTES, &tmA, fb, m0 + 64, k0);
                     }
-                    if constexpr (!B_MN) tma2_load_2d(sB, &tmB, fb, k0, n0);
+                    if constexpr (!B_MN) tma2_load_2d(sB, &tmB, fb, k0 + (KIND == VD_X ? args.k_base : 0), n0);
                     else if (!args.b_split) tma2_load_3d(sB, &tmB, fb, 0, k0, n0 >> 6);
                     else {
                         tma2_load_2d(sB, &tmB, fb, n0, k0);
@@ -165,11 +203,13 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             constexpr uint32_t a_step = (A_MN ? 2048 : 32) >> 4, b_step = (B_MN ? 2048 : 32) >> 4;
             int stage = 0; uint32_t phase = 0; int it = 0; bool alive = true;
             for (int t = cluster_id; t < total && alive; t += n_clusters) {
+                int mt, nt, kb0, kb1;
+                decode(t, mt, nt, kb0, kb1);
                 uint32_t d_tmem = 0;
                 int kseg = 0;                            // K block inside the segment
-                for (int kb = 0; kb < nkb; ++kb) {
-                    if (kb == 0 || (KIND == VD_L && kseg == VD_SEG)) {
-                        if (kb) {                        // segment done: the epilogue adds it up, the next one goes to the other accumulator
+                for (int kb = kb0; kb < kb1; ++kb) {
+                    if (kb == kb0 || (KIND == VD_L && kseg == VD_SEG)) {
+                        if (kb > kb0) {                        // segment done: the epilogue adds it up, the next one goes to the other accumulator
                             if (el) umma2_commit_both(tfull_bar(it & 1));
                             ++it;
                             kseg = 0;
@@ -206,21 +246,20 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         int it = 0;
         bool ok = true;
         for (int t = cluster_id; t < total && ok; t += n_clusters) {
-            int mt, nt;
-            decode(t, mt, nt);
+            int mt, nt, kb0, kb1;
+            decode(t, mt, nt, kb0, kb1);
             const int row = 256 * mt + 128 * (int)rank + quarter * 32 + lane;
             const int col0 = args.n_base + 256 * nt + 128 * half;         // vocabulary column of this thread's first
             if constexpr (KIND == VD_L) {
                 const bool mine = row < args.N;
-                const int32_t* list = args.scol + (size_t)row * args.K;
-                int at = mine ? vd_first(list, args.K, col0) : args.K;
-                int next = at < args.K ? __ldg(list + at) : INT_MAX;
+                VdEntries en;
+                en.open(args, row, 2 * nt + half, mine);
                 float y[4][32];
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
 #pragma unroll
                     for (int i = 0; i < 32; ++i) y[g][i] = 0.0f;
-                const int nseg = (nkb + VD_SEG - 1) / VD_SEG;
+                const int nseg = (kb1 + VD_SEG - 1) / VD_SEG;
                 for (int sg = 0; sg < nseg; ++sg) {
                     if (!mbar_wait_warp(tfull_bar(it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, args.status, STATUS_WAIT_TMEM_FULL,
                                         lane)) { ok = false; break; }
@@ -255,17 +294,16 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 for (int g = 0; g < 4; ++g) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sum += ex2(fmaf(y[g][i], args.c, -mc));
-                    while (next < col0 + 32 * (g + 1)) {  // (entries lie inside the vocabulary)
-                        const int i = next - col0 - 32 * g;
+                    while (en.e[0].x < col0 + 32 * (g + 1)) {             // (entries lie inside the vocabulary)
+                        const int2 e = en.take();
+                        const int i = e.x - col0 - 32 * g;
                         float v = 0.0f;
 #pragma unroll
                         for (int q = 0; q < 32; ++q) v = i == q ? y[g][q] : v;
-                        args.student[(size_t)row * args.K + __ldg(args.sslot + (size_t)row * args.K + at)] = v;
-                        ++at;
-                        next = at < args.K ? __ldg(list + at) : INT_MAX;
+                        args.student[(size_t)row * args.K + e.y] = v;
                     }
                 }
-                if (mine) args.part[(size_t)(2 * nt + half) * args.N + row] = make_float2(m, sum);
+                if (mine) args.part[(size_t)row * args.units + 2 * nt + half] = make_float2(m, sum);
             } else {
                 const bool mine = row < args.N;
                 float coef = 0.0f, lse2 = 0.0f;
@@ -274,15 +312,10 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                     if (mine) coef = args.row_scale[row];
                     if (args.add_to && args.seq_off) inside = row >= __ldg(args.seq_off) && row < __ldg(args.seq_off + args.n_seq);
                 }
-                int at = args.K, next = INT_MAX;
-                const int32_t* list = args.scol + (size_t)row * args.K;
+                VdEntries en;
                 if constexpr (KIND == VD_P) {
-                    if (mine) {
-                        coef = args.coef[row];
-                        lse2 = args.lse2[row];
-                        at = vd_first(list, args.K, col0);
-                        next = at < args.K ? __ldg(list + at) : INT_MAX;
-                    }
+                    if (mine) { coef = args.coef[row]; lse2 = args.lse2[row]; }
+                    en.open(args, row, col0 >> 7, mine);
                 }
                 bool ready = mbar_wait_warp(tfull_bar(it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, args.status, STATUS_WAIT_TMEM_FULL, lane);
                 // the four warps of a column half meet at named barriers below: they give up together or not at all
@@ -300,8 +333,15 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(tempty_bar(it & 1) & T2_PEER_MASK);
                 ++it;
-                uint8_t* box = boxes + half * VD_BOX_BYTES;
-                uint8_t* rowp = box + (quarter * 32 + lane) * 128;
+                if constexpr (KIND == VD_X)
+                    if (args.dx32) {                      // (whole 128-byte lines of 32 columns, a row per lane)
+                        float* out = args.dx32 + ((size_t)(t / tiles) * args.N + row) * args.pitch + col0;
+                        if (mine)
+#pragma unroll
+                            for (int g = 0; g < 4; ++g)
+                                if (col0 + 32 * g < args.pitch) epi_f32<32>(out + 32 * g, y[g], args.accumulate);
+                        continue;
+                    }
                 const bool issuer = quarter == 0 && lane == 0;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {             // 64 columns at a time: a box of 128-byte rows, 16-byte chunks swizzled by row
@@ -322,7 +362,9 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                                 y[g][i + 3] = y[g][i + 3] * s.w * coef;
                             }
                     }
-                    if (issuer) tma_store_wait_read<0>(); // the box's last copy has been read
+                    uint8_t* box = boxes + (2 * half + h) * VD_BOX_BYTES;
+                    uint8_t* rowp = box + (quarter * 32 + lane) * 128;
+                    if (issuer) tma_store_wait_read<1>(); // this box's last copy has been read (the other one's may be on its way)
                     asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
@@ -343,12 +385,11 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                         *reinterpret_cast<uint4*>(rowp + ((j ^ (lane & 7)) << 4)) = o;
                     }
                     if constexpr (KIND == VD_P)
-                        while (next < col0 + 64 * (h + 1)) {              // the teacher's entries among these columns
-                            const int i = next - col0 - 64 * h;
-                            const float v = __ldg(args.sval + (size_t)row * args.K + at);
-                            *reinterpret_cast<bf16*>(rowp + (((i >> 3) ^ (lane & 7)) << 4) + (i & 7) * 2) = __float2bfloat16_rn(v);
-                            ++at;
-                            next = at < args.K ? __ldg(list + at) : INT_MAX;
+                        while (en.e[0].x < col0 + 64 * (h + 1)) {         // the teacher's entries among these columns
+                            const int2 e = en.take();
+                            const int i = e.x - col0 - 64 * h;
+                            *reinterpret_cast<bf16*>(rowp + (((i >> 3) ^ (lane & 7)) << 4) + (i & 7) * 2) =
+                                __float2bfloat16_rn(__int_as_float(e.y));
                         }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
@@ -360,10 +401,11 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 }
             }
         }
-        if (KIND != VD_L && quarter == 0 && lane == 0) tma_store_wait_all();       // boxes read, and written, before the CTA exits
+        if (Tr::STORES && quarter == 0 && lane == 0) tma_store_wait_all();       // boxes read, and written, before the CTA exits
     }
 
     // ------------------------------------------------------------------------- teardown
+    if constexpr (KIND == VD_X) pdl_end_beside();
     tc_fence_before();
     __syncthreads();
     if (*abort_flag) {
@@ -422,11 +464,11 @@ __device__ __forceinline__ void distill_teacher(const DistillLists& l, size_t n,
 
 struct DistillPrep {
     DistillLists l;
-    int32_t* scol; int32_t* sslot; float* sval;                     // sslot forward, sval backward
+    int2* entry; uint16_t* first; int units;                        // as in VdArgs
     float* student_out;                                             // forward: entries outside the vocabulary get 0
     const float* student; const float* lse; const float* dloss;     // backward
     float* coef; float* lse2;
-    int4* tiles; int32_t* n_tiles; int32_t* status;                 // as in vocab_setup_kernel
+    int32_t* status;
 };
 constexpr int DP_WARPS = 8;
 // A warp per row: places every entry by counting the smaller ones (equal columns by their place).  Backward: dY of each entry, the
@@ -437,11 +479,7 @@ __global__ void __launch_bounds__(32 * DP_WARPS) distill_prep_kernel(const Disti
     __shared__ int32_t scols[DP_WARPS][VD_MAX_K];
     __shared__ float sq[DP_WARPS][BWD ? VD_MAX_K : 1];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, N = a.l.N, K = a.l.K;
-    if (blockIdx.x == 0) {
-        const int nt = (N + 255) / 256;
-        for (int i = threadIdx.x; i < nt; i += blockDim.x) a.tiles[i] = make_int4(0, 256 * i, min(256, N - 256 * i), 0);
-        if (threadIdx.x == 0) { *a.n_tiles = nt; *a.status = 0; a.status[VOCAB_NOTE] = 0; }
-    }
+    if (blockIdx.x == 0 && threadIdx.x == 0) { *a.status = 0; a.status[VOCAB_NOTE] = 0; }
     for (int n = blockIdx.x * DP_WARPS + warp; n < N; n += gridDim.x * DP_WARPS) {
         int32_t col[J];
         float q[J], logq[J];
@@ -493,84 +531,84 @@ __global__ void __launch_bounds__(32 * DP_WARPS) distill_prep_kernel(const Disti
         for (int j = 0; j < J; ++j) {
             const int k = lane + 32 * j;
             if (k >= K) continue;
-            const size_t to = (size_t)n * K + rank[j];
-            a.scol[to] = col[j];
-            if constexpr (!BWD) a.sslot[to] = k;
-            else if (col[j] != INT_MAX) {
-                const float p = expf(__fdiv_rn(a.student[(size_t)n * K + k], a.l.tau) - lse);
-                a.sval[to] = g * fmaf(total, p, -same[j]);
+            int2 e = make_int2(col[j], k);
+            if constexpr (BWD)
+                if (col[j] != INT_MAX) {
+                    const float p = expf(__fdiv_rn(a.student[(size_t)n * K + k], a.l.tau) - lse);
+                    e.y = __float_as_int(g * fmaf(total, p, -same[j]));
+                }
+            a.entry[(size_t)n * K + rank[j]] = e;
+        }
+        __syncwarp();                                     // everybody has read the columns: now in order
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+            if (lane + 32 * j < K) scols[warp][rank[j]] = col[j];
+        __syncwarp();
+        for (int u = lane; u <= a.units; u += 32) {
+            int lo = 0, hi = K;
+            while (lo < hi) {
+                const int mid = (lo + hi) >> 1;
+                if (scols[warp][mid] < (long long)u * 128) lo = mid + 1; else hi = mid;
             }
+            a.first[(size_t)n * (a.units + 1) + u] = (uint16_t)lo;
         }
     }
 }
 
-// lse of a row from its (maximum, sum) pairs, then the loss.  A block owns 32 rows (a lane each, its eight warps every eighth pair, as
-// vocab_lse_merge_kernel), then a warp takes four of them, lanes over the entries.
+// A warp per row: lse from the row's (maximum, sum) pairs, then the loss, lanes over the entries.
 struct DistillMerge {
     DistillLists l;
-    const float2* part; int parts;
+    const float2* part; int units;
     const float* student;
     float c;
     float *loss, *lse;
 };
 template <int J>
-__global__ void __launch_bounds__(32 * LSE_WARPS) distill_merge_kernel(const DistillMerge a) {
+__global__ void __launch_bounds__(32 * DP_WARPS) distill_merge_kernel(const DistillMerge a) {
     pdl_begin();
-    __shared__ float2 sh[LSE_WARPS][32];
-    __shared__ float slse[32];
-    const int N = a.l.N, K = a.l.K;
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, n = blockIdx.x * 32 + lane;
-    float M = -INFINITY, S = 0.0f;
-    if (n < N) {
+    const int lane = threadIdx.x % 32, K = a.l.K, n = blockIdx.x * DP_WARPS + threadIdx.x / 32;
+    if (n >= a.l.N) return;
+    const float2* row = a.part + (size_t)n * a.units;
+    float m = -INFINITY, t = 0.0f;
 #pragma unroll 4
-        for (int i = warp; i < a.parts; i += LSE_WARPS) M = fmaxf(M, a.part[(size_t)i * N + n].x);
-        const float Mc = M == -INFINITY ? 0.0f : M * a.c;
+    for (int i = lane; i < a.units; i += 32) m = fmaxf(m, row[i].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    const float mc = m == -INFINITY ? 0.0f : m * a.c;
 #pragma unroll 4
-        for (int i = warp; i < a.parts; i += LSE_WARPS) {
-            const float2 q = a.part[(size_t)i * N + n];
-            S += q.y * exp2f(q.x == -INFINITY ? -INFINITY : fmaf(q.x, a.c, -Mc));
-        }
+    for (int i = lane; i < a.units; i += 32) {
+        const float2 q = row[i];
+        t += q.y * exp2f(fmaf(q.x, a.c, -mc));            // (a unit behind the last column: 0 x 2^-inf)
     }
-    sh[warp][lane] = make_float2(M, S);
-    __syncthreads();
-    if (warp == 0) {
-        float m = sh[0][lane].x;
 #pragma unroll
-        for (int w = 1; w < LSE_WARPS; ++w) m = fmaxf(m, sh[w][lane].x);
-        const float mc = m == -INFINITY ? 0.0f : m * a.c;
-        float t = 0.0f;
+    for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    const float lse = __fdiv_rn(m, a.l.tau) + logf(t);
+    int32_t col[J];
+    float q[J], logq[J], sum = 0.0f;
+    distill_teacher<J>(a.l, n, lane, col, q, logq);
 #pragma unroll
-        for (int w = 0; w < LSE_WARPS; ++w)
-            if (w < a.parts) t += sh[w][lane].y * exp2f(sh[w][lane].x == -INFINITY ? -INFINITY : fmaf(sh[w][lane].x, a.c, -mc));
-        const float l = __fdiv_rn(m, a.l.tau) + logf(t);
-        slse[lane] = l;
-        if (n < N) a.lse[n] = l;
-    }
-    __syncthreads();
-    for (int r = warp; r < 32; r += LSE_WARPS) {
-        const int row = blockIdx.x * 32 + r;
-        if (row >= N) break;
-        int32_t col[J];
-        float q[J], logq[J], sum = 0.0f;
-        distill_teacher<J>(a.l, row, lane, col, q, logq);
+    for (int j = 0; j < J; ++j)
+        if (q[j] != 0.0f) sum += q[j] * (logq[j] - __fdiv_rn(a.student[(size_t)n * K + lane + 32 * j], a.l.tau) + lse);
 #pragma unroll
-        for (int j = 0; j < J; ++j)
-            if (q[j] != 0.0f) sum += q[j] * (logq[j] - __fdiv_rn(a.student[(size_t)row * K + lane + 32 * j], a.l.tau) + slse[r]);
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (lane == 0) a.loss[row] = sum;
-    }
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) { a.lse[n] = lse; a.loss[n] = sum; }
 }
 
-// dX from its fp32 sums [N, pitch], 8 elements a thread.
-__global__ void __launch_bounds__(256) distill_dx_kernel(const float* __restrict__ src, bf16* __restrict__ dst, int N, int H, int pitch) {
+// dX from its fp32 sums [splits, N, pitch], added in order, 8 elements a thread.
+__global__ void __launch_bounds__(256) distill_dx_kernel(const float* __restrict__ src, bf16* __restrict__ dst, int N, int H, int pitch,
+                                                         int splits) {
     pdl_begin();
     const int per = H / 8;
     const size_t n8 = (size_t)N * per;
     for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < n8; i += (size_t)gridDim.x * blockDim.x) {
         const size_t r = i / per, c = (i - r * per) * 8;
-        const float4 a = *reinterpret_cast<const float4*>(src + r * pitch + c), b = *reinterpret_cast<const float4*>(src + r * pitch + c + 4);
-        const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+        float v[8] = {};
+#pragma unroll 4
+        for (int s = 0; s < splits; ++s) {
+            const float4* p = reinterpret_cast<const float4*>(src + ((size_t)s * N + r) * pitch + c);
+            const float4 a = p[0], b = p[1];
+            v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+        }
         store_bf16_run<8>(dst + r * H + c, v);
     }
 }
@@ -578,7 +616,7 @@ __global__ void __launch_bounds__(256) distill_dx_kernel(const float* __restrict
 // ------------------------------------------------------------------------------------------ host
 template <int KIND>
 inline mop_status vd_set_smem() {
-    return cudaFuncSetAttribute(vd_gemm_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, VD_SMEM_BYTES) == cudaSuccess
+    return cudaFuncSetAttribute(vd_gemm_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, VdTraits<KIND>::SMEM_BYTES) == cudaSuccess
                ? MOP_OK : MOP_ERR_CUDA;
 }
 inline mop_status vd_init() {
@@ -586,17 +624,41 @@ inline mop_status vd_init() {
     if ((r = vd_set_smem<VD_L>()) != MOP_OK) return r;
     if ((r = vd_set_smem<VD_P>()) != MOP_OK) return r;
     if ((r = vd_set_smem<VD_R>()) != MOP_OK) return r;
+    if ((r = vd_set_smem<VD_X>()) != MOP_OK) return r;
     return vd_set_smem<VD_W>();
 }
 template <int KIND>
 inline mop_status vd_launch(const TcPlan* p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const VdArgs& args,
                             cudaStream_t st) {
-    return pdl_launch(vd_gemm_kernel<KIND>, p->sm_count & ~1, VD_THREADS, VD_SMEM_BYTES, st, a, b, o, args) == cudaSuccess ? MOP_OK
+    return pdl_launch(vd_gemm_kernel<KIND>, p->sm_count & ~1, VD_THREADS, VdTraits<KIND>::SMEM_BYTES, st, a, b, o, args) == cudaSuccess ? MOP_OK
                                                                                                                       : MOP_ERR_CUDA;
 }
 // 2-D map over `cols` columns of a bf16 matrix whose rows are `pitch` elements apart, for stores; box = {64 columns, 128 rows}.
 inline bool vd_map_out(const TcPlan* p, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch) {
     return tc_map_2d_pitch(p, m, base, rows, cols, pitch, 128);
+}
+
+// Vocabulary columns whose logit gradients are live at a time: as many as keep dY at 2^26 elements (128 MiB), at least 8192, in blocks
+// of about equal width.  Wide blocks mean few launches, long sums and few passes over the fp32 sums of dX.
+constexpr long long VD_LIVE = 1ll << 26;
+inline int vd_block(int N, int V) {
+    const long long most = VD_LIVE / N > 8192 ? VD_LIVE / N : 8192;
+    const int blocks = (int)((V + most - 1) / most);
+    return (int)(((long long)(V + blocks - 1) / blocks + 255) / 256 * 256);
+}
+// Ranges of K of the dX product, by the makespan of the round-robin over the pairs in microseconds: a K block of a tile takes 0.3, a
+// unit 2 more, and each range its sums' way to L2 and back.
+constexpr int VD_MAX_SPLITS = 16, VD_PAIRS = 74;
+inline int vd_splits(int N, int H, int width) {
+    const int tiles = ((N + 255) / 256) * ((H + 255) / 256), kb = (width + 63) / 64;
+    const double t_sum = 8e-6 * N * H / 5.0;
+    int pick = 1;
+    double best = 1e30;
+    for (int s = 1; s <= VD_MAX_SPLITS && s <= kb; ++s) {
+        const double t = ((tiles * (long long)s + VD_PAIRS - 1) / VD_PAIRS) * (((kb + s - 1) / s) * 0.3 + 2.0) + (s > 1 ? t_sum * s : 0.0);
+        if (t < 0.97 * best) { best = t; pick = s; }
+    }
+    return pick;
 }
 
 #define DISTILL_BY_K(K, GO)                                       \

@@ -1865,25 +1865,26 @@ mop_status mop_vocab_loss_bwd(int device, int32_t N, int32_t H, int32_t V, const
 // Distillation from a teacher's top logits through the same projection
 // ---------------------------------------------------------------------------------------------
 namespace {
-struct DistillLayout { size_t status, tiles, scol, sslot, sval, coef, lse2, part, dy, dx32, total; int vc, hp; };
+struct DistillLayout { size_t status, entry, first, coef, lse2, part, dy, dx32, total; int units, vc, blocks, splits, pitch; };
 DistillLayout distill_layout(int N, int H, int V, int K, bool backward) {
     DistillLayout L{};
     size_t o = 0;
     auto take = [&](size_t b) { size_t r = o; o += align_up(b); return r; };
+    L.units = 2 * ceil_div(V, 256);
     L.status = take(256);                 // first: mop_vocab_poll reads it without knowing the shape
-    L.tiles = take(tc_tile_table_bytes(N, 1));
-    L.scol = take((size_t)N * K * 4);
+    L.entry = take((size_t)N * K * 8);
+    L.first = take((size_t)N * (L.units + 1) * 2);
     if (!backward) {
-        L.sslot = take((size_t)N * K * 4);
-        L.part = take((size_t)ceil_div(V, 256) * 2 * N * 8);
-    } else {
-        L.vc = V < kVocabBlock ? ceil_div(V, 64) * 64 : kVocabBlock;
-        L.hp = ceil_div(H, 32) * 32;      // dX is added up in whole runs of 32 columns
-        L.sval = take((size_t)N * K * 4);
+        L.part = take((size_t)L.units * N * 8);
+    } else if (N > 0) {
+        L.vc = vd_block(N, V);
+        L.blocks = ceil_div(V, L.vc);
+        L.splits = vd_splits(N, H, V < L.vc ? V : L.vc);
+        L.pitch = ceil_div(H, 32) * 32;   // dX is added up in whole runs of 32 columns
         L.coef = take((size_t)N * 4);
         L.lse2 = take((size_t)N * 4);
         L.dy = take((size_t)N * L.vc * 2);
-        L.dx32 = take((size_t)N * L.hp * 4);
+        if (L.blocks > 1 || L.splits > 1) L.dx32 = take((size_t)L.splits * N * L.pitch * 4);
     }
     L.total = o;
     return L;
@@ -1926,14 +1927,13 @@ mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, in
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const DistillLayout L = distill_layout(N, H, V, K, false);
     char* w = static_cast<char*>(workspace);
-    int32_t* tiles = reinterpret_cast<int32_t*>(w + L.tiles);
     CUtensorMap mX, mW;
     if (!tc_map_2d(p, &mX, X, N, H, 128) || !distill_map_mn(p, &mW, W_voc, H, V)) return MOP_ERR_CUDA;
     const DistillLists lists = {teacher_idx, teacher_logits, teacher_lse_opt, N, V, K, temperature};
     DistillPrep a{};
-    a.l = lists; a.scol = reinterpret_cast<int32_t*>(w + L.scol); a.sslot = reinterpret_cast<int32_t*>(w + L.sslot);
+    a.l = lists; a.entry = reinterpret_cast<int2*>(w + L.entry); a.first = reinterpret_cast<uint16_t*>(w + L.first); a.units = L.units;
     a.student_out = student;
-    a.tiles = reinterpret_cast<int4*>(tiles + 64); a.n_tiles = tiles; a.status = reinterpret_cast<int32_t*>(w + L.status);
+    a.status = reinterpret_cast<int32_t*>(w + L.status);
     const int blocks = min(ceil_div(N, DP_WARPS), p->sm_count * 8);
 #define GO(J) pdl_launch(distill_prep_kernel<J, false>, blocks, 32 * DP_WARPS, 0, st, a)
     DISTILL_BY_K(K, GO);
@@ -1942,12 +1942,12 @@ mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, in
     g.N = N; g.H = H; g.V = V; g.K = K;
     g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(V, 256); g.n_group = VOCAB_N_GROUP; g.kblocks = ceil_div(H, TC_BK);
     g.cols = V; g.b_split = V % 64 != 0; g.c = (float)(1.4426950408889634 / temperature);
-    g.scol = a.scol; g.sslot = a.sslot; g.student = student; g.part = reinterpret_cast<float2*>(w + L.part);
+    g.splits = 1; g.entry = a.entry; g.first = a.first; g.units = L.units; g.student = student; g.part = reinterpret_cast<float2*>(w + L.part);
     g.status = a.status;
     if ((r = vd_launch<VD_L>(p, mX, mW, mW, g, st)) != MOP_OK) return r;
     DistillMerge m{};
-    m.l = lists; m.part = g.part; m.parts = 2 * g.tiles_n; m.student = student; m.c = g.c; m.loss = loss; m.lse = lse;
-#define GO(J) pdl_launch(distill_merge_kernel<J>, ceil_div(N, 32), 32 * LSE_WARPS, 0, st, m)
+    m.l = lists; m.part = g.part; m.units = L.units; m.student = student; m.c = g.c; m.loss = loss; m.lse = lse;
+#define GO(J) pdl_launch(distill_merge_kernel<J>, ceil_div(N, DP_WARPS), 32 * DP_WARPS, 0, st, m)
     DISTILL_BY_K(K, GO);
 #undef GO
     return cudaGetLastError() == cudaSuccess ? MOP_OK : MOP_ERR_CUDA;
@@ -1976,20 +1976,19 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
     if ((r = vocab_plan(device, &p)) != MOP_OK) return r;
     const DistillLayout L = distill_layout(N, H, V, K, true);
     char* w = static_cast<char*>(workspace);
-    int32_t* tiles = reinterpret_cast<int32_t*>(w + L.tiles);
     int32_t* status = reinterpret_cast<int32_t*>(w + L.status);
     bf16* dY = reinterpret_cast<bf16*>(w + L.dy);
-    float* dx32 = reinterpret_cast<float*>(w + L.dx32);
-    CUtensorMap mX, mXT, mWn, mWk;
+    float* dx32 = L.blocks > 1 || L.splits > 1 ? reinterpret_cast<float*>(w + L.dx32) : nullptr;
+    CUtensorMap mX, mXT, mWn, mWk, mdX;
     if (!tc_map_2d(p, &mX, X, N, H, 128) || !distill_map_mn(p, &mXT, X, N, H) || !distill_map_mn(p, &mWn, W_voc, H, V) ||
-        !tc_map_3d(p, &mWk, W_voc, 1, H, V, 128))
+        !tc_map_2d(p, &mWk, W_voc, H, V, 128) || !vd_map_out(p, &mdX, dX, N, H, H))
         return MOP_ERR_CUDA;
     DistillPrep a{};
     a.l = {teacher_idx, teacher_logits, teacher_lse_opt, N, V, K, temperature};
-    a.scol = reinterpret_cast<int32_t*>(w + L.scol); a.sval = reinterpret_cast<float*>(w + L.sval);
+    a.entry = reinterpret_cast<int2*>(w + L.entry); a.first = reinterpret_cast<uint16_t*>(w + L.first); a.units = L.units;
     a.student = student; a.lse = lse; a.dloss = dloss;
     a.coef = reinterpret_cast<float*>(w + L.coef); a.lse2 = reinterpret_cast<float*>(w + L.lse2);
-    a.tiles = reinterpret_cast<int4*>(tiles + 64); a.n_tiles = tiles; a.status = status;
+    a.status = status;
     const int blocks = min(ceil_div(N, DP_WARPS), p->sm_count * 8);
 #define GO(J) pdl_launch(distill_prep_kernel<J, true>, blocks, 32 * DP_WARPS, 0, st, a)
     DISTILL_BY_K(K, GO);
@@ -2000,14 +1999,16 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
         if (!tc_map_2d_pitch(p, &mdYk, dY, N, cw, L.vc, 128) || !tc_map_chunked_2d_pitch(p, &mdYn, dY, N, cw64, L.vc, 2) ||
             !vd_map_out(p, &mdYo, dY, N, L.vc, L.vc) || !vd_map_out(p, &mdW, static_cast<bf16*>(dW_voc) + c0, H, cw, V))
             return MOP_ERR_CUDA;
-        const PdlNote note = {status + VOCAB_NOTE, c0 / L.vc + 1};
+        const bool last = c0 + L.vc >= V;
         VdArgs base{};
-        base.N = N; base.H = H; base.V = V; base.K = K; base.n_group = VOCAB_N_GROUP; base.status = status; base.gemm_follows = true;
+        base.N = N; base.H = H; base.V = V; base.K = K; base.n_group = VOCAB_N_GROUP; base.splits = 1; base.status = status;
+        base.gemm_follows = true;
+        const PdlNote note = {status + VOCAB_NOTE, c0 / L.vc + 1};
         {   // dY block, logits formed again on the tensor cores
             VdArgs g = base;
             g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(cw, 256); g.kblocks = ceil_div(H, TC_BK);
             g.n_base = c0; g.cols = cw64; g.b_split = V % 64 != 0; g.c = (float)(1.4426950408889634 / temperature);
-            g.scol = a.scol; g.sval = a.sval; g.coef = a.coef; g.lse2 = a.lse2;
+            g.entry = a.entry; g.first = a.first; g.units = L.units; g.coef = a.coef; g.lse2 = a.lse2;
             if ((r = vd_launch<VD_P>(p, mX, mWn, mdYo, g, st)) != MOP_OK) return r;
         }
         {   // dW[:, block] = X^T dY (K = the N tokens), written once
@@ -2016,20 +2017,19 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
             g.cols = cw; g.a_split = H % 64 != 0; g.note = note;
             if ((r = vd_launch<VD_W>(p, mXT, mdYn, mdW, g, st)) != MOP_OK) return r;
         }
-        {   // dX += dY W[:, block]^T in fp32 across the blocks, beside the weight gradient (as in mop_vocab_loss_bwd)
-            TcArgs g{};
-            g.n_mtiles = tiles; g.n_group = VOCAB_N_GROUP; g.mtiles = reinterpret_cast<const int4*>(tiles + 64);
-            g.E = 1; g.status = status; g.ep.M_total = N;
-            g.note = note;
-            g.gemm_follows = c0 + L.vc < V;
-            g.tiles_n = ceil_div(H, 256); g.kblocks = ceil_div(cw, TC_BK); g.N = L.hp; g.kb_base = c0;
-            g.ep.outf = dx32; g.ep.accumulate = c0 > 0 ? 1 : 0;
-            if ((r = tc2_launch<TC_VX>(p, "vocab_dgrad", mdYk, mdYk, mWk, mWk, g, st)) != MOP_OK) return r;
+        {   // dX (+)= dY W[:, block]^T, its CTAs take over from those of the weight gradient (as in mop_vocab_loss_bwd)
+            VdArgs g = base;
+            g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(H, 256); g.kblocks = ceil_div(cw, TC_BK); g.k_base = c0;
+            g.splits = min(L.splits, g.kblocks);          // (the first block is the widest and writes the sums of every range)
+            g.cols = H; g.dx32 = dx32; g.pitch = L.pitch; g.accumulate = c0 > 0 ? 1 : 0;
+            g.note = note; g.gemm_follows = !last;        // the small blocks that follow the last one must not pile up
+            if ((r = vd_launch<VD_X>(p, mdYk, mWk, mdX, g, st)) != MOP_OK) return r;
         }
     }
+    if (!dx32) return MOP_OK;
     const size_t n8 = (size_t)N * (H / 8), cap = (size_t)p->sm_count * 16;
     pdl_launch(distill_dx_kernel, (unsigned)((n8 + 255) / 256 < cap ? (n8 + 255) / 256 : cap), 256, 0, st, dx32, static_cast<bf16*>(dX), N,
-               H, L.hp);
+               H, L.pitch, L.splits);
     return cudaGetLastError() == cudaSuccess ? MOP_OK : MOP_ERR_CUDA;
 }
 

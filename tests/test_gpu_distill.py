@@ -81,8 +81,8 @@ SHAPES = [
     (1, 64, 64, 3, 2.0, True, 1.0),
     (300, 128, 1024, 17, 1.0, False, 1.0),
     (129, 200, 328, 32, 1.5, False, 1.0),                # neither width a multiple of 64
-    (257, 328, 8192 + 200, 64, 2.0, True, 1.0),          # two vocabulary blocks, the second of one tile
-    (513, 256, 16384 + 72, 33, 4.0, False, 0.3),         # three
+    (257, 328, 8192 + 200, 64, 2.0, True, 1.0),
+    (513, 256, 16384 + 72, 33, 4.0, False, 0.3),         # dX in several ranges of its columns
     (64, 1032, 4160, 100, 1.0, True, 1.0),               # five segments of K, the last of one block that is nearly empty
     (37, 72, 1000, 256, 0.5, False, 0.1),                # the longest lists, all within 100 columns: places named many times
     (1100, 136, 520, 128, 1.0, False, 1.0),
@@ -159,10 +159,10 @@ def test_a_logit_that_is_not_finite_shows_in_the_loss(column, value):
     assert torch.isfinite(loss[~lost]).all()
 
 
-@pytest.mark.parametrize("N", [200, 1100])
-def test_nothing_is_taken_from_what_the_workspace_held(N):
-    """Three blocks of columns: the same bits whether the workspaces hold NaN, small counts or another call's sums, back to back."""
-    H, V, K = 256, 2 * 8192 + 72, 40
+@pytest.mark.parametrize("N,H", [(200, 256), (8200, 72)], ids=["one-block", "three-blocks"])
+def test_nothing_is_taken_from_what_the_workspace_held(N, H):
+    """The same bits whether the workspaces hold NaN, small counts or another call's sums, calls back to back."""
+    V, K = 2 * 8192 + 72, 40
     calls = []
     for seed in (1, 2):
         X, W, ids, t, dloss = inputs(N, H, V, K, seed=seed)
@@ -231,6 +231,28 @@ def test_nothing_is_written_outside_the_outputs_and_the_workspaces():
     check_backward(X, W, ids, t, 1.0, None, dloss, dX, dW)
     for whole, n in fences:
         assert bool((whole[:margin] == 0xA5).all()) and bool((whole[margin + n:] == 0xA5).all())
+
+
+@pytest.mark.parametrize("N,H,V", [(8200, 72, 16384 + 72),        # three blocks of columns, the last one shorter and of no whole chunk
+                                   (8193, 328, 8192 + 8),         # two
+                                   (700, 2048, 4096)],            # one block, dX in one range: stored at once
+                         ids=lambda v: str(v))
+def test_blocks_of_columns_against_fp64_on_the_device(N, H, V):
+    K, tau = 50, 1.5
+    X, W, ids, t, dloss = inputs(N, H, V, K, seed=N)
+    loss, student, lse, _ = forward(X, W, ids, t, tau)
+    dX, dW, _ = backward(X, W, ids, t, tau, student, lse, dloss)
+    Y = X.double() @ W.double()
+    ref = torch.logsumexp(Y / tau, 1)
+    far = SUM_TOL * float((X.double().abs().max() * W.double().abs().sum(0).max()).item())
+    assert float((lse.double() - ref).abs().max()) <= far / tau + 4e-6 + 2.0 ** -22 * float(ref.abs().max())
+    q = torch.softmax(t.double() / tau, 1)
+    want_loss = (q * (q.log() - Y.gather(1, ids.long()) / tau + ref[:, None])).sum(1)
+    assert float((loss.double() - want_loss).abs().max()) <= 2 * far / tau + 4e-6 + 3e-6 * float(ref.abs().max())
+    dY = torch.softmax(Y / tau, 1).scatter_add_(1, ids.long(), -q) * (dloss.double() / tau)[:, None]
+    for got, want, terms in ((dX, dY @ W.double().T, dY.abs() @ W.double().abs().T), (dW, X.double().T @ dY, X.double().abs().T @ dY.abs())):
+        err = (got.double() - want).abs()
+        assert bool((err <= 2.0 ** -8 * want.abs() + 2.0 ** -7 * terms).all()) and float(err.norm() / want.norm()) <= 4e-3
 
 
 def test_full_size_sampled_rows_and_invariant():
