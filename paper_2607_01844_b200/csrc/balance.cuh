@@ -10,7 +10,7 @@
 //
 // The two products of the backward have T d E multiply-adds each (60 GFLOP at T = 16384, d = 7168, E = 256) and run on the tensor cores:
 //   dW_r = x^T dz   must have fp32 accuracy: dz goes in as three bf16 pieces (24 bits), x is bf16 already (bal_dw_pair_kernel)
-//   dX = dz W_r^T   is rounded to bf16: both operands go in as fp16 (11 bits), each row scaled by its own power of two, so that
+//   dX = dz W_r^T   is rounded to bf16: both operands go in as fp16 (11 bits), a token's row and 32 rows of W_r scaled by a power of two, so that
 //                   neither the size of the upstream weight nor that of the router's weights matters (vd_gemm_kernel<VD_R>)
 #pragma once
 #include <cuda_fp16.h>
@@ -238,13 +238,14 @@ struct BalBwdArgs {
     const float* logits; const float* bias; const int32_t* counts; const float* dloss;
     BalSeqs q; BalShape s;
     int chunk, dz_blocks;
+    int32_t* note;                        // cleared here: the word of the PdlNote between the two products
     float* dz;                            // [T, E] fp32, or null
     float* dbias_part;                    // [dz_blocks][E], or null
     // for the tensor cores, each or null:
     int Ep;                               // columns of the buffers below: E rounded up to 64, zeros behind it
     bf16* pieces;                         // [3][T][Ep]: dz = hi + mid + lo
     __half* dz16; float* row_scale;       // [T][Ep], [T]: dz = dz16 row_scale
-    const float* W_r; __half* w16; float* col_scale; int d;      // [d][Ep], [d]: W_r = w16 col_scale, by the blocks behind dz_blocks
+    const float* W_r; __half* w16; float* col_scale; int d;      // [d][Ep], [d / 32]: W_r = w16 col_scale, by the blocks behind dz_blocks
     const uint4* x; uint4* xe;            // [128][d]: the first and last 64 tokens of the sequences' range, see bal_dw_pair_kernel
 };
 constexpr int BAL_EDGE_BLOCKS = 8;        // blocks for each of the two edges of x
@@ -262,22 +263,28 @@ __device__ __forceinline__ uint2 bal_half4(const float* v, float by) {
     const __half2 a = __floats2half2_rn(v[0] * by, v[1] * by), b = __floats2half2_rn(v[2] * by, v[3] * by);
     return make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
 }
-// A warp per row of W_r: fp16 with the row's scale.
+// 32 rows of W_r a block: fp16 with one scale for all of them (a row that is 2^-28 of its neighbours would lose digits).
 __device__ __forceinline__ void bal_convert_w(const BalBwdArgs& a, int block, int blocks) {
-    const int lane = threadIdx.x % 32, warps = blockDim.x / 32;
-    for (int r = block * warps + threadIdx.x / 32; r < a.d; r += blocks * warps) {
-        const float* row = a.W_r + (size_t)r * a.s.E;
+    __shared__ float amax_of[16];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, warps = blockDim.x / 32, E = a.s.E;
+    for (int r0 = block * 32; r0 < a.d; r0 += blocks * 32) {
         float amax = 0.0f, up, down;
-        for (int e = lane; e < a.s.E; e += 32) amax = fmaxf(amax, fabsf(row[e]));
+        for (int r = r0 + warp; r < min(r0 + 32, a.d); r += warps)
+            for (int e = lane; e < E; e += 32) amax = fmaxf(amax, fabsf(a.W_r[(size_t)r * E + e]));
         for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+        __syncthreads();
+        if (lane == 0) amax_of[warp] = amax;
+        __syncthreads();
+        for (int w = 0; w < warps; ++w) amax = fmaxf(amax, amax_of[w]);
         bal_scale(amax, up, down);
-        for (int e = 4 * lane; e < a.Ep; e += 128) {
-            float v[4];
+        for (int r = r0 + warp; r < min(r0 + 32, a.d); r += warps)
+            for (int e = 4 * lane; e < a.Ep; e += 128) {
+                float v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = e + i < a.s.E ? row[e + i] : 0.0f;
-            *reinterpret_cast<uint2*>(a.w16 + (size_t)r * a.Ep + e) = bal_half4(v, up);
-        }
-        if (lane == 0) a.col_scale[r] = down;
+                for (int i = 0; i < 4; ++i) v[i] = e + i < E ? a.W_r[(size_t)r * E + e + i] : 0.0f;
+                *reinterpret_cast<uint2*>(a.w16 + (size_t)r * a.Ep + e) = bal_half4(v, up);
+            }
+        if (threadIdx.x == 0) a.col_scale[r0 / 32] = down;
     }
 }
 // Blocks of 64 tokens that the range [begin, end) of the sequences covers in part only: the padding in them must not meet the
@@ -299,9 +306,10 @@ __device__ __forceinline__ void bal_copy_edge(const BalBwdArgs& a, int edge, int
 // change by a shift, and under a nearly balanced load, which this loss aims at, the difference keeps its digits.
 // The blocks behind the first dz_blocks prepare W_r and the edges of x.
 template <int NV>
-__global__ void __launch_bounds__(NV == 8 ? 256 : 512) balance_dz_kernel(const BalBwdArgs a) {
+__global__ void __launch_bounds__(256) balance_dz_kernel(const BalBwdArgs a) {
     pdl_begin();
     extern __shared__ float bal_smem[];                                   // [W][E]
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.note = 0;
     if ((int)blockIdx.x >= a.dz_blocks) {
         int b = (int)blockIdx.x - a.dz_blocks;
         if (a.xe) {
@@ -322,30 +330,44 @@ __global__ void __launch_bounds__(NV == 8 ? 256 : 512) balance_dz_kernel(const B
         bias[i] = a.bias && e < s.E ? a.bias[e] : 0.0f;
         acc[i] = 0.0f;
     }
+    // the lane's sequence, and what follows from it, as long as its tokens stay inside
+    int first = 0, last = 0;
+    float w = 0.0f, c[4 * NV], next[4 * NV];
+    bal_load<NV>(a.logits + (size_t)(c0 + warp * tpw + group) * s.E, s, e0, c0 + warp * tpw + group < c1, next);
     for (int tb = c0 + warp * tpw; tb < c1; tb += W * tpw) {
         const int t = tb + group;
-        int seq = bal_find(a.q, tb, lane);
-        while (seq < a.q.S && t >= bal_off(a.q, seq + 1)) ++seq;
-        const bool on = t < c1 && seq >= 0 && seq < a.q.S;
-        float z[4 * NV], oms[4 * NV], c[4 * NV];
-        bal_load<NV>(a.logits + (size_t)t * s.E, s, e0, on, z);
-        float w = 0.0f, dot = 0.0f;
-        int32_t shift = 0;
-        if (on) {
-            const float n = (float)max(1, bal_off(a.q, seq + 1) - bal_off(a.q, seq));
-            w = a.dloss[seq] * ((float)s.E / (float)s.k) / (n * n);
-            shift = (int32_t)rintf(n * (float)s.k / (float)s.E);
+        float z[4 * NV], oms[4 * NV], dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4 * NV; ++i) z[i] = next[i];
+        bal_load<NV>(a.logits + (size_t)(t + W * tpw) * s.E, s, e0, t + W * tpw < c1, next);
+        if (__any_sync(0xffffffffu, t < c1 && !(t >= first && t < last))) {
+            int seq = bal_find(a.q, tb, lane);
+            while (seq < a.q.S && t >= bal_off(a.q, seq + 1)) ++seq;
+            const bool in = t < c1 && seq >= 0 && seq < a.q.S;
+            first = last = 0;
+            int32_t shift = 0;
+            if (in) {
+                first = bal_off(a.q, seq); last = bal_off(a.q, seq + 1);
+                const float n = (float)max(1, last - first);
+                w = a.dloss[seq] * ((float)s.E / (float)s.k) / (n * n);
+                shift = (int32_t)rintf(n * (float)s.k / (float)s.E);
+            }
+#pragma unroll
+            for (int i = 0; i < 4 * NV; ++i) {
+                const int e = e0 + 4 * s.G * (i / 4) + i % 4;
+                c[i] = in && e < s.E ? (float)(a.counts[(size_t)seq * s.E + e] - shift) : 0.0f;
+            }
         }
+        const bool on = t >= first && t < last && t < c1;
+        if (!on)
+#pragma unroll
+            for (int i = 0; i < 4 * NV; ++i) z[i] = -INFINITY;            // (a padding token's logits may be anything)
         if (a.bias)
 #pragma unroll
             for (int i = 0; i < 4 * NV; ++i) z[i] += bias[i];
         bal_scores<NV>(s, z, oms);
 #pragma unroll
-        for (int i = 0; i < 4 * NV; ++i) {
-            const int e = e0 + 4 * s.G * (i / 4) + i % 4;
-            c[i] = on && e < s.E ? (float)(a.counts[(size_t)seq * s.E + e] - shift) : 0.0f;
-            dot = fmaf(z[i], c[i], dot);
-        }
+        for (int i = 0; i < 4 * NV; ++i) dot = fmaf(z[i], c[i], dot);
         dot = bal_sum(dot, s.G);
         float amax = 0.0f;
 #pragma unroll
@@ -417,18 +439,46 @@ __global__ void __launch_bounds__(NV == 8 ? 256 : 512) balance_dz_kernel(const B
 // dW_r on CTA pairs: 256 rows of dW_r x up to 256 experts, K = the tokens.  As in route_score_pair_kernel, what bounds such a product
 // of three pieces is the traffic into shared memory, so a 64-token block of x (both operands lie with their columns contiguous) is
 // fetched once and multiplied with that block of all three pieces; x and the pieces travel through separate rings; and the K loop
-// is added up in segments of BW_SEG blocks, because the tensor core truncates where it adds.  The tokens are cut into `splits` ranges,
-// separate units of work whose sums balance_dw_sum_kernel adds in order.
+// is added up in segments of BW_SEG blocks, because the tensor core truncates where it adds.
+//
+// Few tiles, long sums: the token blocks of all tiles are laid in a row and cut into equal ranges, one for each pair.  A tile that one
+// range covers goes to dW_r at once; of one that is cut, each range leaves its sums, and balance_dw_sum_kernel adds them in order.
+// T 16384, d 7168, E 256: 28 tiles of 256 blocks are 97 blocks for each pair (five equal ranges per tile made 104, and 140 sums).
 constexpr int BW_SA = 3, BW_SB = 9, BW_SLOT = 16384, BW_SEG = 3, BW_EPI_WARPS = 8;
 constexpr int BW_THREADS = 64 + 32 * BW_EPI_WARPS;
 constexpr int BW_SMEM_BYTES = (BW_SA + BW_SB) * BW_SLOT + 1024 /*align*/ + TC_BAR_BYTES;
+// The row of token blocks in units of half a block of 256 experts (a last tile of at most 128 experts costs half): the tiles of 256
+// experts, row tiles fastest, then the narrow ones.
+struct BalCut {
+    int tiles_m, wide, narrow, kb;        // row tiles, tiles of 256 experts, 0 or 1 narrow one, token blocks
+    int range;                            // units of a pair
+    __host__ __device__ int tiles() const { return tiles_m * (wide + narrow); }
+    __host__ __device__ bool is_wide(int tile) const { return tile < tiles_m * wide; }
+    __host__ __device__ int cost(int tile) const { return is_wide(tile) ? 2 * kb : kb; }
+    __host__ __device__ int start(int tile) const {
+        return is_wide(tile) ? tile * 2 * kb : tiles_m * wide * 2 * kb + (tile - tiles_m * wide) * kb;
+    }
+    __host__ __device__ int total() const { return start(tiles()); }
+    __host__ __device__ int tile_at(int unit) const {
+        const int w = tiles_m * wide * 2 * kb;
+        return unit < w ? unit / (2 * kb) : tiles_m * wide + (unit - w) / kb;
+    }
+    __host__ __device__ int first_pair(int tile) const { return start(tile) / range; }
+    __host__ __device__ int last_pair(int tile) const { return (start(tile) + cost(tile) - 1) / range; }
+    // token block at which a unit of the tile lies (every block belongs to exactly one range)
+    __host__ __device__ int block_at(int tile, int unit) const { return is_wide(tile) ? (unit - start(tile) + 1) / 2 : unit - start(tile); }
+};
 struct BalDwArgs {
     BalSeqs q;
-    int T, d, E, splits;
-    float* out;            // splits == 1: dW_r; else the sums of the ranges, [splits][d][E]
-    int accumulate;        // splits == 1: add to dW_r
+    BalCut cut;
+    int T, d, E;
+    float* dW;
+    float* part;           // [pairs][2][256][256]: sums of cut tiles, slot 0 of one that began in an earlier range, 1 of one that goes on
+    int accumulate;
     int x_split;           // d is no multiple of 64: one copy per 64-wide chunk of x, whose edge is zero-filled
     int32_t* status;
+    bool gemm_follows;
+    PdlNote note;
 };
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(BW_THREADS, 1)
@@ -470,26 +520,25 @@ bal_dw_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
     cluster_sync_all();          // the peer's barriers exist before anything signals them
     tc_fence_after();
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-    pdl_begin();
+    pdl_begin_gemm(args.gemm_follows, args.note);
 
     const int begin = bal_off(args.q, 0), end = bal_off(args.q, args.q.S);
     const int kb_first = begin / TC_BK, kblocks = end > begin ? (end - 1) / TC_BK + 1 - kb_first : 0;
-    const int tiles_n = (args.E + 255) / 256, tiles_m = (args.d + 255) / 256;
-    const int total = tiles_m * tiles_n * args.splits;
-    const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+    const BalCut cut = args.cut;
+    const int pair = blockIdx.x >> 1;
+    const int unit0 = min(cut.total(), pair * cut.range), unit1 = min(cut.total(), unit0 + cut.range);
     // columns of n-tile nt: 256, or 128 for a last tile of at most 128 columns
     auto tile_cols = [&](int nt) { return (args.E - 256 * nt <= 128) ? 128 : 256; };
-    // unit of work -> rows of dW_r, experts, token blocks; the row tiles of one token range are neighbours and read the same pieces
-    struct Unit { int mt, nt, ks, kb0, kb1; };
-    auto decode = [&](int t) {
+    // the part of a tile that lies in this pair's range: rows of dW_r, experts, token blocks (of those that hold any tokens)
+    struct Unit { int tile, mt, nt, kb0, kb1, next; };
+    auto decode = [&](int unit) {
         Unit u;
-        u.mt = t % tiles_m;
-        t /= tiles_m;
-        u.nt = t % tiles_n;
-        u.ks = t / tiles_n;
-        const int per = (kblocks + args.splits - 1) / args.splits;
-        u.kb0 = kb_first + min(kblocks, u.ks * per);
-        u.kb1 = kb_first + min(kblocks, (u.ks + 1) * per);
+        u.tile = cut.tile_at(unit);
+        u.mt = u.tile % cut.tiles_m;
+        u.nt = u.tile / cut.tiles_m;
+        u.next = min(unit1, cut.start(u.tile) + cut.cost(u.tile));
+        u.kb0 = max(kb_first, cut.block_at(u.tile, unit));
+        u.kb1 = max(u.kb0, min(kb_first + kblocks, cut.block_at(u.tile, u.next)));
         return u;
     };
 
@@ -497,8 +546,9 @@ bal_dw_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
         // ===================================================================== TMA producer (both CTAs)
         const bool el = elect_one();
         int sa = 0, sb = 0; uint32_t pa = 0, pb = 0; bool alive = true;
-        for (int t = cluster_id; t < total && alive; t += n_clusters) {
+        for (int t = unit0, to; t < unit1 && alive; t = to) {
             const Unit u = decode(t);
+            to = u.next;
             const int m0 = u.mt * 256 + 128 * (int)rank;          // past d: the copy fills zeros
             const int half_cols = tile_cols(u.nt) >> 1;           // this CTA's columns: 64 or 128
             const int chunk0 = (u.nt * 256 + (int)rank * half_cols) >> 6;
@@ -538,8 +588,9 @@ bal_dw_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
             const uint64_t desc = smem_desc(0, TC_CHUNK_BYTES, 1024);
             constexpr uint32_t step = 2048 >> 4;        // 16 rows of K, 128 bytes each
             int sa = 0, sb = 0; uint32_t pa = 0, pb = 0; int it = 0; bool alive = true;
-            for (int t = cluster_id; t < total && alive; t += n_clusters) {
+            for (int t = unit0, to; t < unit1 && alive; t = to) {
                 const Unit u = decode(t);
+                to = u.next;
                 if (u.kb0 >= u.kb1) continue;
                 const uint32_t idesc = idesc0 | ((uint32_t)(tile_cols(u.nt) >> 3) << 17);
                 uint32_t d_tmem = 0;
@@ -586,8 +637,9 @@ bal_dw_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
         const int half = (warp - 2) >> 2;        // columns [128*half, 128*half + 128) of the tile
         int it = 0;
         bool ok = true;
-        for (int t = cluster_id; t < total && ok; t += n_clusters) {
+        for (int t = unit0, to; t < unit1 && ok; t = to) {
             const Unit u = decode(t);
+            to = u.next;
             const int nseg = (u.kb1 - u.kb0 + BW_SEG - 1) / BW_SEG;
             const bool active = half * 128 < tile_cols(u.nt);
             float sum[4][32];
@@ -612,34 +664,38 @@ bal_dw_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(tempty_bar(b) & T2_PEER_MASK);
+                if (lane == 0) mbar_arrive_pair(tempty_bar(b) & T2_PEER_MASK);
                 ++it;
             }
             if (!ok) break;
             const int row = u.mt * 256 + 128 * (int)rank + quarter * 32 + lane;
-            if (active && row < args.d) {
-                float* out = args.out + ((size_t)u.ks * args.d + row) * args.E;
-                const bool add = args.accumulate && args.splits == 1;
+            if (!active || row >= args.d) continue;
+            const bool whole = cut.first_pair(u.tile) == cut.last_pair(u.tile);
+            const int col = u.nt * 256 + half * 128;
+            if (!whole) {                        // (rows of 256 columns, whatever the number of experts)
+                float* out = args.part + ((size_t)pair * 2 + (cut.first_pair(u.tile) < pair ? 0 : 1)) * 65536 +
+                             (size_t)(128 * (int)rank + quarter * 32 + lane) * 256 + half * 128;
 #pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const int col = u.nt * 256 + half * 128 + 32 * g;
-                    if (args.E % 4 == 0) {
+                for (int g = 0; g < 4; ++g) epi_f32<32>(out + 32 * g, sum[g], 0);
+            } else if (args.E % 4 == 0) {
+                float* out = args.dW + (size_t)row * args.E + col;
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            if (col + i >= args.E) continue;
-                            float4 v = make_float4(sum[g][i], sum[g][i + 1], sum[g][i + 2], sum[g][i + 3]);
-                            if (add) {
-                                const float4 o = *reinterpret_cast<const float4*>(out + col + i);
-                                v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
-                            }
-                            *reinterpret_cast<float4*>(out + col + i) = v;
-                        }
-                    } else {
+                for (int g = 0; g < 4; ++g)
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (col + i < args.E) out[col + i] = add ? out[col + i] + sum[g][i] : sum[g][i];
+                    for (int i = 0; i < 32; i += 4) {
+                        if (col + 32 * g + i >= args.E) continue;
+                        float4 v = make_float4(sum[g][i], sum[g][i + 1], sum[g][i + 2], sum[g][i + 3]);
+                        float4* o = reinterpret_cast<float4*>(out + 32 * g + i);
+                        if (args.accumulate) { v.x += o->x; v.y += o->y; v.z += o->z; v.w += o->w; }
+                        *o = v;
                     }
-                }
+            } else {
+                float* out = args.dW + (size_t)row * args.E + col;
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (col + 32 * g + i < args.E) out[32 * g + i] = args.accumulate ? out[32 * g + i] + sum[g][i] : sum[g][i];
             }
         }
     }
@@ -659,31 +715,56 @@ bal_dw_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
     }
 }
 
-// The ranges' sums, added in order.
-__global__ void __launch_bounds__(256) balance_dw_sum_kernel(const float* __restrict__ part, float* __restrict__ dW, size_t n, int splits,
-                                                             int accumulate) {
+// The sums of the tiles that are cut, added in order, four experts a thread; and, by the blocks behind the first dw_blocks, the bias's
+// gradient: 32 experts a block, its eight warps every eighth part.
+struct BalSumArgs {
+    BalCut cut;
+    int d, E, dw_blocks;
+    const float* part; float* dW;
+    const float* dbias_part; float* dbias; int dbias_parts;
+    int accumulate;
+};
+__global__ void __launch_bounds__(256) balance_sum_kernel(const BalSumArgs a) {
     pdl_begin();
-    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; 4 * i < n; i += (size_t)gridDim.x * blockDim.x) {
-        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        float4* o = reinterpret_cast<float4*>(dW) + i;       // (n = d E is a multiple of 4: d is one of 8)
-#pragma unroll 4
-        for (int s = 0; s < splits; ++s) {
-            const float4 p = reinterpret_cast<const float4*>(part + s * n)[i];
-            v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
-        }
-        if (accumulate) { v.x += o->x; v.y += o->y; v.z += o->z; v.w += o->w; }
-        *o = v;
+    if ((int)blockIdx.x >= a.dw_blocks) {
+        __shared__ float sh[8][32];
+        const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, e = ((int)blockIdx.x - a.dw_blocks) * 32 + lane;
+        float v = 0.0f;
+        if (e < a.E)
+#pragma unroll 8
+            for (int b = warp; b < a.dbias_parts; b += 8) v += a.dbias_part[(size_t)b * a.E + e];
+        sh[warp][lane] = v;
+        __syncthreads();
+        if (warp || e >= a.E) return;
+        for (int w = 1; w < 8; ++w) v += sh[w][lane];
+        a.dbias[e] = a.accumulate ? a.dbias[e] + v : v;
+        return;
     }
-}
-
-__global__ void __launch_bounds__(256) balance_dbias_kernel(const float* __restrict__ part, float* __restrict__ dbias, int blocks, int E,
-                                                            int accumulate) {
-    pdl_begin();
-    const int e = blockIdx.x * blockDim.x + threadIdx.x;
-    if (e >= E) return;
-    float v = 0.0f;
-    for (int b = 0; b < blocks; ++b) v += part[(size_t)b * E + e];
-    dbias[e] = accumulate ? dbias[e] + v : v;
+    const int E4 = (a.E + 3) / 4;
+    const size_t n = (size_t)a.d * E4;
+    for (size_t i = blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)a.dw_blocks * 256) {
+        const int row = (int)(i / E4), e = (int)(i - (size_t)row * E4) * 4;
+        const int tile = (e >> 8) * a.cut.tiles_m + (row >> 8), p0 = a.cut.first_pair(tile), p1 = a.cut.last_pair(tile);
+        if (p0 == p1) continue;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const float* at = a.part + (size_t)(row & 255) * 256 + (e & 255);
+#pragma unroll 4
+        for (int p = p0; p <= p1; ++p) {
+            const float4 s = *reinterpret_cast<const float4*>(at + ((size_t)p * 2 + (p == p0 ? 1 : 0)) * 65536);
+            v.x += s.x; v.y += s.y; v.z += s.z; v.w += s.w;
+        }
+        float* o = a.dW + (size_t)row * a.E + e;
+        if (a.E % 4 == 0) {
+            float4* o4 = reinterpret_cast<float4*>(o);
+            if (a.accumulate) { v.x += o4->x; v.y += o4->y; v.z += o4->z; v.w += o4->w; }
+            *o4 = v;
+        } else {
+            const float r[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (e + j < a.E) o[j] = a.accumulate ? o[j] + r[j] : r[j];
+        }
+    }
 }
 
 // The same products on the CUDA cores, for contexts whose GEMMs run there (MOP_GEMM_SCALAR).
@@ -758,11 +839,16 @@ __global__ void __launch_bounds__(256) balance_dx_kernel(const float* __restrict
 }
 
 // ------------------------------------------------------------------------------------------ host
-constexpr int BAL_MAX_SPLITS = 16;
 constexpr int BAL_PAIRS = 74;             // CTA pairs that the rules below count with (148 SMs)
 // Tokens per block: one block for each SM, at least 16 tokens each.
 inline int bal_chunk(int T) { const int c = (T + 147) / 148; return c < 16 ? 16 : c; }
 inline int bal_blocks(int T) { return (T + bal_chunk(T) - 1) / bal_chunk(T); }
+// ... of the backward: eight warps, one round of tokens for each of about 600 blocks.
+inline int bal_chunk_bwd(int T, int E) {
+    const int round = 8 * (E <= 64 ? 2 : 1), c = (T + 591) / 592;
+    return c < round ? round : c;
+}
+inline int bal_blocks_bwd(int T, int E) { return (T + bal_chunk_bwd(T, E) - 1) / bal_chunk_bwd(T, E); }
 inline int bal_warps(int E) { return E <= 512 ? 16 : 8; }
 inline size_t bal_smem_bytes(int E, int warps) { return (size_t)(warps + 1) * E * 4; }
 inline BalShape bal_shape(const mop_moe_shape& s) {
@@ -774,20 +860,27 @@ inline mop_status bal_init() {
     if (cudaFuncSetAttribute(bal_dw_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BW_SMEM_BYTES) != cudaSuccess) return MOP_ERR_CUDA;
     return vd_set_smem<VD_R>();
 }
-// Token ranges of the dW_r product: the makespan of the round-robin over the pairs, in microseconds.  A token block of a tile takes 0.8
-// (256 experts) or 0.4, a unit 2.5 more to fill its rings and store its tile, and a further range costs its sums' way to L2 and back.
-inline int bal_splits(int T, int d, int E, int pairs) {
-    const int tiles = ((d + 255) / 256) * ((E + 255) / 256), kb = (T + 63) / 64;
-    const double t_kb = E <= 128 ? 0.4 : 0.8, t_sum = 8e-6 * d * E / 5.0;
-    int pick = 1;
-    double best = 1e30;
-    for (int s = 1; s <= BAL_MAX_SPLITS && s <= kb; ++s) {
-        const int rounds = (tiles * s + pairs - 1) / pairs;
-        const double t = rounds * (((kb + s - 1) / s) * t_kb + 2.5) + (s > 1 ? 3.0 + t_sum * s : 0.0);
-        if (t < best) { best = t; pick = s; }
-    }
-    return pick;
+// Ranges of the dW_r product: equal shares of the row of token blocks, at least 8 blocks each, if that is worth the further launch and
+// the sums' way to L2 and back (about 6 us) against whole tiles: a token block of 256 experts takes 0.8 us.
+inline BalCut bal_cut(int T, int d, int E) {
+    BalCut c{};
+    const int rest = E % 256;
+    c.tiles_m = (d + 255) / 256; c.kb = (T + 63) / 64;
+    c.narrow = rest > 0 && rest <= 128 ? 1 : 0;
+    c.wide = (E + 255) / 256 - c.narrow;
+    const int most = c.wide ? 2 * c.kb : c.kb, per_block = c.wide ? 2 : 1, total = c.total();
+    int share = (total + BAL_PAIRS - 1) / BAL_PAIRS;
+    if (share < 8 * per_block) share = 8 * per_block;
+    const int whole = (c.tiles() + BAL_PAIRS - 1) / BAL_PAIRS * most;
+    c.range = (whole - share) * 0.4 > 6.0 ? share : whole;
+    return c;
 }
+inline bool bal_is_cut(const BalCut& c) {
+    for (int t = 0; t < c.tiles(); ++t)
+        if (c.first_pair(t) != c.last_pair(t)) return true;
+    return false;
+}
+constexpr size_t BAL_PART_BYTES = (size_t)BAL_PAIRS * 2 * 65536 * 4;
 #define BAL_BY_WIDTH(E, GO)                                       \
     do {                                                          \
         if ((E) <= 128) GO(1);                                    \

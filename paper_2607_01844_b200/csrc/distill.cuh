@@ -23,12 +23,14 @@ namespace mop {
 
 enum : int { VD_L = 0, VD_P = 1, VD_W = 2, VD_R = 3, VD_X = 4 };
 
-// Stages, and store boxes (128 rows x 64 bf16 columns) for each column half: one is read by the copy engine while the next is filled.
+// Stages, and store boxes (128 rows x 64 bf16 columns) for each column half: a tile fills two.  The router's product has a short
+// main loop (its K are the experts), so its boxes are there twice: one pair is read by the copy engine while the next is filled.
 template <int KIND>
 struct VdTraits {
     static constexpr bool STORES = KIND != VD_L;
-    static constexpr int BOXES = STORES ? 2 : 0;
-    static constexpr int STAGES = STORES ? 5 : 6;
+    static constexpr int SETS = KIND == VD_R ? 2 : 1;         // pairs of boxes
+    static constexpr int BOXES = STORES ? 2 * SETS : 0;
+    static constexpr int STAGES = KIND == VD_L ? 6 : KIND == VD_R ? 3 : 5;
     static constexpr int SMEM_BYTES = STAGES * T2_STAGE_BYTES + 2 * BOXES * 16384 + 1024 /*align*/ + TC_BAR_BYTES;
 };
 constexpr int VD_EPI_WARPS = 8;
@@ -36,7 +38,7 @@ constexpr int VD_THREADS = 64 + 32 * VD_EPI_WARPS;
 constexpr int VD_BOX_BYTES = 128 * 64 * 2;
 // K blocks (of 64) per accumulation segment of the forward.  The tensor core truncates where it adds; a segment starts from zero and
 // the finished ones are added in fp32 registers, rounding to nearest.
-constexpr int VD_SEG = 4;
+constexpr int VD_SEG = 8;
 constexpr int VD_MAX_K = 256;                                 // entries of a teacher's list
 
 struct VdArgs {
@@ -55,7 +57,7 @@ struct VdArgs {
     float2* part;                 // VD_L: [N, units] (maximum, sum)
     const float* coef;            // VD_P: dloss / tau Q per row
     const float* lse2;            // VD_P: log-sum-exp per row in units of log 2
-    const float *row_scale, *col_scale;   // VD_R: what undoes the operands' scaling, per token and per column of dX
+    const float *row_scale, *col_scale;   // VD_R: what undoes the operands' scaling, per token and per 32 columns of dX
     bf16* add_to;                 // VD_R: dX [N, cols] that the product is added to, or null
     const int32_t* seq_off;       // VD_R: offsets of the sequences or null: rows outside [seq_off[0], seq_off[n_seq]) keep what they hold
     int n_seq;
@@ -65,6 +67,12 @@ struct VdArgs {
     bool gemm_follows;
     PdlNote note;
 };
+
+// "TMEM has been read": nothing in memory is published by it, so the arrival releases at CTA scope only.  (At cluster scope every
+// arrival waits for the thread's own global stores first: the largest stall of the segmented loops.)
+__device__ __forceinline__ void mbar_arrive_pair(uint32_t bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 
 __device__ __forceinline__ float ex2(float v) {
     float r;
@@ -140,8 +148,10 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     cluster_sync_all();          // the peer's barriers exist before anything signals them
     tc_fence_after();
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-    // dX runs beside the weight gradient of its block: both read the logit gradients, neither what the other writes.
-    if constexpr (KIND == VD_X) pdl_begin_beside(args.gemm_follows, args.note);
+    // dX runs beside the weight gradient (of its block): both read the logit gradients, neither what the other writes.
+    constexpr bool BESIDE = KIND == VD_X || KIND == VD_R;
+    const bool beside = BESIDE && args.note.word;
+    if (beside) pdl_begin_beside(args.gemm_follows, args.note);
     else pdl_begin_gemm(args.gemm_follows, args.note);
 
     const int tiles = args.tiles_m * args.tiles_n, total = KIND == VD_X ? tiles * args.splits : tiles;
@@ -273,7 +283,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster(tempty_bar(it & 1) & T2_PEER_MASK);
+                    if (lane == 0) mbar_arrive_pair(tempty_bar(it & 1) & T2_PEER_MASK);
                     ++it;
                 }
                 if (!ok) break;
@@ -308,8 +318,12 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 const bool mine = row < args.N;
                 float coef = 0.0f, lse2 = 0.0f;
                 bool inside = true;
+                float scale[4] = {};
+                (void)scale;
                 if constexpr (KIND == VD_R) {
                     if (mine) coef = args.row_scale[row];
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) scale[g] = __ldg(args.col_scale + col0 / 32 + g);
                     if (args.add_to && args.seq_off) inside = row >= __ldg(args.seq_off) && row < __ldg(args.seq_off + args.n_seq);
                 }
                 VdEntries en;
@@ -331,7 +345,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 tmem_ld_wait4(y[0], y[1], y[2], y[3]);
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(tempty_bar(it & 1) & T2_PEER_MASK);
+                if (lane == 0) mbar_arrive_pair(tempty_bar(it & 1) & T2_PEER_MASK);
                 ++it;
                 if constexpr (KIND == VD_X)
                     if (args.dx32) {                      // (whole 128-byte lines of 32 columns, a row per lane)
@@ -343,46 +357,47 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                         continue;
                     }
                 const bool issuer = quarter == 0 && lane == 0;
+                const int set = Tr::SETS == 2 ? (it - 1) & 1 : 0;
+                uint8_t* box = boxes + (Tr::BOXES * half + 2 * set) * VD_BOX_BYTES;
+                if constexpr (KIND == VD_P) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {             // 64 columns at a time: a box of 128-byte rows, 16-byte chunks swizzled by row
-                    if constexpr (KIND == VD_P)
+                    for (int g = 0; g < 4; ++g)
 #pragma unroll
-                        for (int g = 2 * h; g < 2 * h + 2; ++g)
+                        for (int i = 0; i < 32; ++i) y[g][i] = coef * ex2(fmaf(y[g][i], args.c, -lse2));
+                }
+                if constexpr (KIND == VD_R) {
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) y[g][i] = coef * ex2(fmaf(y[g][i], args.c, -lse2));
-                    if constexpr (KIND == VD_R) {
+                    for (int g = 0; g < 4; ++g) {
+                        scale[g] *= coef;
 #pragma unroll
-                        for (int g = 2 * h; g < 2 * h + 2; ++g)
-#pragma unroll
-                            for (int i = 0; i < 32; i += 4) {
-                                const float4 s = __ldg(reinterpret_cast<const float4*>(args.col_scale + col0 + 32 * g + i));
-                                y[g][i] = y[g][i] * s.x * coef;
-                                y[g][i + 1] = y[g][i + 1] * s.y * coef;
-                                y[g][i + 2] = y[g][i + 2] * s.z * coef;
-                                y[g][i + 3] = y[g][i + 3] * s.w * coef;
-                            }
+                        for (int i = 0; i < 32; ++i) y[g][i] *= scale[g];
                     }
-                    uint8_t* box = boxes + (2 * half + h) * VD_BOX_BYTES;
-                    uint8_t* rowp = box + (quarter * 32 + lane) * 128;
-                    if (issuer) tma_store_wait_read<1>(); // this box's last copy has been read (the other one's may be on its way)
-                    asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+                    if (args.add_to && mine) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float* v = &y[2 * h + j / 4][(j % 4) * 8];
-                        uint4 o;
-                        if constexpr (KIND == VD_R) {
-                            const int col = col0 + 64 * h + 8 * j;
-                            if (args.add_to && mine && col < args.cols) {
-                                o = *reinterpret_cast<const uint4*>(args.add_to + (size_t)row * args.cols + col);
-                                if (inside) {
-                                    v[0] += bf16_lo(o.x); v[1] += bf16_hi(o.x); v[2] += bf16_lo(o.y); v[3] += bf16_hi(o.y);
-                                    v[4] += bf16_lo(o.z); v[5] += bf16_hi(o.z); v[6] += bf16_lo(o.w); v[7] += bf16_hi(o.w);
-                                }
+                        for (int j = 0; j < 16; ++j) {
+                            if (col0 + 8 * j >= args.cols) continue;
+                            float* v = &y[j / 4][(j % 4) * 8];
+                            const uint4 o = *reinterpret_cast<const uint4*>(args.add_to + (size_t)row * args.cols + col0 + 8 * j);
+                            if (inside) {
+                                v[0] += bf16_lo(o.x); v[1] += bf16_hi(o.x); v[2] += bf16_lo(o.y); v[3] += bf16_hi(o.y);
+                                v[4] += bf16_lo(o.z); v[5] += bf16_hi(o.z); v[6] += bf16_lo(o.w); v[7] += bf16_hi(o.w);
+                            } else {                      // (the rounding below gives back the same bits)
+                                v[0] = bf16_lo(o.x); v[1] = bf16_hi(o.x); v[2] = bf16_lo(o.y); v[3] = bf16_hi(o.y);
+                                v[4] = bf16_lo(o.z); v[5] = bf16_hi(o.z); v[6] = bf16_lo(o.w); v[7] = bf16_hi(o.w);
                             }
                         }
-                        if (KIND != VD_R || inside)
-                            o = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
-                        *reinterpret_cast<uint4*>(rowp + ((j ^ (lane & 7)) << 4)) = o;
+                    }
+                }
+                if (issuer) tma_store_wait_read<Tr::SETS - 1>();          // this pair's last copies have been read
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {             // boxes of 128-byte rows, 16-byte chunks swizzled by row
+                    uint8_t* rowp = box + h * VD_BOX_BYTES + (quarter * 32 + lane) * 128;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float* v = &y[2 * h + j / 4][(j % 4) * 8];
+                        *reinterpret_cast<uint4*>(rowp + ((j ^ (lane & 7)) << 4)) =
+                            make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
                     }
                     if constexpr (KIND == VD_P)
                         while (en.e[0].x < col0 + 64 * (h + 1)) {         // the teacher's entries among these columns
@@ -391,13 +406,16 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                             *reinterpret_cast<bf16*>(rowp + (((i >> 3) ^ (lane & 7)) << 4) + (i & 7) * 2) =
                                 __float2bfloat16_rn(__int_as_float(e.y));
                         }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
-                    if (issuer) {
-                        const int x = 256 * nt + 128 * half + 64 * h, r0 = 256 * mt + 128 * (int)rank;
-                        if (x < args.cols && r0 < (KIND == VD_W ? args.H : args.N)) tma_store_2d(&tmO, smem_u32(box), x, r0);
-                        tma_store_commit();
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+                if (issuer) {
+                    const int x = 256 * nt + 128 * half, r0 = 256 * mt + 128 * (int)rank;
+                    if (r0 < (KIND == VD_W ? args.H : args.N)) {
+                        if (x < args.cols) tma_store_2d(&tmO, smem_u32(box), x, r0);
+                        if (x + 64 < args.cols) tma_store_2d(&tmO, smem_u32(box + VD_BOX_BYTES), x + 64, r0);
                     }
+                    tma_store_commit();
                 }
             }
         }
@@ -405,7 +423,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     }
 
     // ------------------------------------------------------------------------- teardown
-    if constexpr (KIND == VD_X) pdl_end_beside();
+    if (beside) pdl_end_beside();
     tc_fence_before();
     __syncthreads();
     if (*abort_flag) {

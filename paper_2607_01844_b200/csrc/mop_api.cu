@@ -1158,7 +1158,7 @@ mop_status mop_moe_route_bwd(mop_ctx* c, const float* logits, const float* bias,
 // Load-balance loss of the router and its gradients (the caller owns the workspace)
 // ---------------------------------------------------------------------------------------------
 namespace {
-struct BalanceLayout { size_t part_p, part_c, dz, dbias, pieces, dz16, row_scale, w16, col_scale, xe, dw_part, total; };
+struct BalanceLayout { size_t part_p, part_c, dz, dbias, pieces, dz16, row_scale, w16, col_scale, xe, dw_part, note, total; };
 BalanceLayout balance_layout(const mop_moe_shape& s, bool backward) {
     BalanceLayout L{};
     size_t o = 0;
@@ -1168,7 +1168,8 @@ BalanceLayout balance_layout(const mop_moe_shape& s, bool backward) {
         L.part_p = take(2 * blocks * E * 4);
         L.part_c = take(2 * blocks * E * 4);
     } else {
-        L.dbias = take(blocks * E * 4);
+        L.note = take(256);
+        L.dbias = take((size_t)bal_blocks_bwd(s.T, s.E) * E * 4);
         if (s.gemm_path == MOP_GEMM_SCALAR) {
             L.dz = take(T * E * 4);
         } else {
@@ -1176,10 +1177,9 @@ BalanceLayout balance_layout(const mop_moe_shape& s, bool backward) {
             L.dz16 = take(T * Ep * 2);
             L.row_scale = take(T * 4);
             L.w16 = take(d * Ep * 2);
-            L.col_scale = take((d + 255) / 256 * 1024);
+            L.col_scale = take((d + 255) / 256 * 32);     // (8 of 32 columns for every 256)
             L.xe = take(128 * d * 2);
-            const int splits = bal_splits(s.T, s.d, s.E, BAL_PAIRS);
-            if (splits > 1) L.dw_part = take((size_t)splits * d * E * 4);
+            if (s.T > 0 && bal_is_cut(bal_cut(s.T, s.d, s.E))) L.dw_part = take(BAL_PART_BYTES);
         }
     }
     L.total = o;
@@ -1261,10 +1261,11 @@ mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logi
     BalBwdArgs a{};
     a.logits = logits; a.bias = pre ? bias : nullptr; a.counts = counts; a.dloss = dloss;
     a.q = {seq_offsets, n_seq, s.T}; a.s = bal_shape(s); a.s.G = bal_group_bwd(s.E);
-    a.chunk = bal_chunk(s.T); a.dz_blocks = bal_blocks(s.T);
+    a.chunk = bal_chunk_bwd(s.T, s.E); a.dz_blocks = bal_blocks_bwd(s.T, s.E);
+    a.note = reinterpret_cast<int32_t*>(w + L.note);
     a.dz = dlogits_opt;
     a.dbias_part = pre && dbias_opt ? reinterpret_cast<float*>(w + L.dbias) : nullptr;
-    const int warps = bal_warps(s.E);
+    const int warps = 8;
     int extra = 0;
     if (tensor) {
         a.Ep = bal_ep(s.E); a.d = s.d;
@@ -1276,7 +1277,7 @@ mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logi
         if (dX_opt) {
             a.dz16 = reinterpret_cast<__half*>(w + L.dz16); a.row_scale = reinterpret_cast<float*>(w + L.row_scale);
             a.W_r = W_r; a.w16 = reinterpret_cast<__half*>(w + L.w16); a.col_scale = reinterpret_cast<float*>(w + L.col_scale);
-            extra += min(ceil_div(s.d, warps), 2 * c->sm_count);
+            extra += min(ceil_div(s.d, 32), 2 * c->sm_count);
         }
     } else if (!a.dz && (dW_r_opt || dX_opt)) a.dz = reinterpret_cast<float*>(w + L.dz);
 #define GO(NV) pdl_launch(balance_dz_kernel<NV>, a.dz_blocks + extra, 32 * warps, bal_smem_bytes(s.E, warps), st, a)
@@ -1284,30 +1285,28 @@ mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logi
 #undef GO
     mop_status r = after_launch(c);
     if (r != MOP_OK) return r;
-    if (a.dbias_part) {
-        LAUNCH(c, "balance_dbias", st,
-               pdl_launch(balance_dbias_kernel, ceil_div(s.E, 256), 256, 0, st, a.dbias_part, dbias_opt, a.dz_blocks, s.E, accumulate));
-        if ((r = after_launch(c)) != MOP_OK) return r;
-    }
+    BalSumArgs sum{};
+    sum.d = s.d; sum.E = s.E; sum.accumulate = accumulate;
+    sum.dbias_part = a.dbias_part; sum.dbias = dbias_opt; sum.dbias_parts = a.dz_blocks;
+    const int dbias_blocks = a.dbias_part ? ceil_div(s.E, 32) : 0;
+    PdlNote note{};
     if (dW_r_opt && tensor) {
         BalDwArgs g{};
-        g.q = a.q; g.T = s.T; g.d = s.d; g.E = s.E; g.splits = bal_splits(s.T, s.d, s.E, BAL_PAIRS);
-        g.out = g.splits > 1 ? reinterpret_cast<float*>(w + L.dw_part) : dW_r_opt;
+        g.q = a.q; g.cut = bal_cut(s.T, s.d, s.E); g.T = s.T; g.d = s.d; g.E = s.E; g.dW = dW_r_opt;
+        const bool is_cut = bal_is_cut(g.cut);
+        if (is_cut) g.part = reinterpret_cast<float*>(w + L.dw_part);
         g.accumulate = accumulate; g.x_split = s.d % 64 != 0; g.status = c->status;
+        if (dX_opt) note = {a.note, 1};
+        g.note = note; g.gemm_follows = dX_opt != nullptr;
         CUtensorMap mX, mXe, mP2, mP1;
         if (!tc_map_mn(&c->plan, &mX, x, s.T, s.d, 2) || !tc_map_mn(&c->plan, &mXe, a.xe, 128, s.d, 2) ||
             !tc_map_chunked_3d(&c->plan, &mP2, a.pieces, 3, s.T, a.Ep, 2) || !tc_map_chunked_3d(&c->plan, &mP1, a.pieces, 3, s.T, a.Ep, 1))
             return MOP_ERR_CUDA;
         LAUNCH(c, "balance_dw", st,
-               pdl_launch(bal_dw_pair_kernel, c->sm_count & ~1, BW_THREADS, BW_SMEM_BYTES, st, mX, mXe, mP2, mP1, g));
+               pdl_launch(bal_dw_pair_kernel, 2 * ceil_div(g.cut.total(), g.cut.range), BW_THREADS, BW_SMEM_BYTES, st, mX, mXe, mP2, mP1, g));
         if ((r = after_launch(c)) != MOP_OK) return r;
-        if (g.splits > 1) {
-            const size_t n = (size_t)s.d * s.E;
-            LAUNCH(c, "balance_dw_sum", st,
-                   pdl_launch(balance_dw_sum_kernel, (unsigned)min((n / 4 + 255) / 256, (size_t)c->sm_count * 8), 256, 0, st, g.out,
-                              dW_r_opt, n, g.splits, accumulate));
-            if ((r = after_launch(c)) != MOP_OK) return r;
-        }
+        sum.cut = g.cut; sum.part = g.part; sum.dW = dW_r_opt;
+        if (is_cut) sum.dw_blocks = (int)min(((size_t)s.d * ((s.E + 3) / 4) + 255) / 256, (size_t)c->sm_count * 8);
     } else if (dW_r_opt) {
         LAUNCH(c, "balance_dw", st,
                pdl_launch(balance_dw_kernel, dim3(ceil_div(s.d, 64), ceil_div(s.E, 64)), 256, 0, st, static_cast<const bf16*>(x), a.dz,
@@ -1316,10 +1315,10 @@ mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logi
     }
     if (dX_opt && tensor) {
         VdArgs g{};
-        g.N = s.T; g.H = s.d; g.tiles_m = ceil_div(s.T, 256); g.tiles_n = ceil_div(s.d, 256); g.n_group = g.tiles_n;
+        g.N = s.T; g.H = s.d; g.tiles_m = ceil_div(s.T, 256); g.tiles_n = ceil_div(s.d, 256); g.n_group = g.tiles_n; g.splits = 1;
         g.kblocks = a.Ep / TC_BK; g.cols = s.d; g.row_scale = a.row_scale; g.col_scale = a.col_scale;
         g.add_to = accumulate ? static_cast<bf16*>(dX_opt) : nullptr; g.seq_off = seq_offsets; g.n_seq = n_seq;
-        g.status = c->status;
+        g.status = c->status; g.note = note;
         CUtensorMap mA, mB, mO;
         if (!tc_map_2d(&c->plan, &mA, a.dz16, s.T, a.Ep, 128) || !tc_map_2d(&c->plan, &mB, a.w16, s.d, a.Ep, 128) ||
             !vd_map_out(&c->plan, &mO, dX_opt, s.T, s.d, s.d))
@@ -1330,6 +1329,10 @@ mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logi
         LAUNCH(c, "balance_dx", st,
                pdl_launch(balance_dx_kernel, dim3(ceil_div(s.d, 64), ceil_div(s.T, 64)), 256, 0, st, a.dz, W_r, a.q,
                           static_cast<bf16*>(dX_opt), s.T, s.d, s.E, accumulate));
+        r = after_launch(c);
+    }
+    if (r == MOP_OK && sum.dw_blocks + dbias_blocks > 0) {
+        LAUNCH(c, "balance_sum", st, pdl_launch(balance_sum_kernel, sum.dw_blocks + dbias_blocks, 256, 0, st, sum));
         r = after_launch(c);
     }
     return r;
