@@ -11,7 +11,7 @@
 // The two products of the backward have T d E multiply-adds each (60 GFLOP at T = 16384, d = 7168, E = 256) and run on the tensor cores:
 //   dW_r = x^T dz   must have fp32 accuracy: dz goes in as three bf16 pieces (24 bits), x is bf16 already (bal_dw_pair_kernel)
 //   dX = dz W_r^T   is rounded to bf16: both operands go in as fp16 (11 bits), a token's row and 32 rows of W_r scaled by a power of two, so that
-//                   neither the size of the upstream weight nor that of the router's weights matters (vd_gemm_kernel<VD_R>)
+//                   neither the size of the upstream weight nor that of the router's weights matters (vd_gemm_kernel, kind VD_R)
 #pragma once
 #include <cuda_fp16.h>
 
@@ -858,7 +858,7 @@ inline BalShape bal_shape(const mop_moe_shape& s) {
 inline int bal_group_bwd(int E) { return E <= 64 ? 16 : 32; }
 inline mop_status bal_init() {
     if (cudaFuncSetAttribute(bal_dw_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, BW_SMEM_BYTES) != cudaSuccess) return MOP_ERR_CUDA;
-    return vd_set_smem<VD_R>();
+    return vd_set_smem<VD_R, VD_PAIR>();
 }
 // Ranges of the dW_r product: equal shares of the row of token blocks, at least 8 blocks each, if that is worth the further launch and
 // the sums' way to L2 and back (about 6 us) against whole tiles: a token block of 256 experts takes 0.8 us.

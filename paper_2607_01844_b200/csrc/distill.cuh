@@ -4,15 +4,17 @@
 //   loss[n] = sum_k q_k (log q_k - s[n, i_k] + lse[n])
 //   dY[n,v] = dloss[n] / tau (Q p[n,v] - sum_{k: i_k = v} q_k),   p = exp(s - lse),   Q = sum_k q_k
 //
-// vd_gemm_kernel runs the products on CTA pairs (256 x 256 tiles, tcgen05.mma.cta_group::2, stages of 64 of K, as
-// tc_gemm2_kernel), with eight epilogue warps:
-//   VD_L  Y = X W_voc: per row and 128 columns the maximum and the sum of exponentials, and the logits of the teacher's entries
+// vd_gemm_kernel runs the products, with eight epilogue warps behind a TMA producer and an MMA issuer:
+//   VD_L  Y = X W_voc: per row and up to 128 columns the maximum and the sum of exponentials, and the logits of the teacher's entries
 //   VD_P  dY, one block of vocabulary columns, bf16 (the only piece of the N x V matrix that ever exists)
 //   VD_W  dW_voc[:, block] = X^T dY, bf16
 //   VD_X  dX = dY W_voc^T, beside VD_W: the block's columns (its K) in `splits` ranges, fp32 sums over the blocks
-//   VD_R  the router's dX (+)= dz W_r^T (balance.cuh) from fp16 operands whose rows are scaled by powers of two, bf16
+//   VD_R  the router's dX (+)= dz W_r^T (balance.cuh) from fp16 operands that are scaled by powers of two, bf16
+// With many rows on CTA pairs (256 x 256 tiles, tcgen05.mma.cta_group::2, stages of 64 of K, as tc_gemm2_kernel).  With up to 128 rows
+// a pair would multiply as much again in vain, and half of its stages would hold X: reading W is all there is then, and the product
+// runs on single CTAs, tiles of 128 rows and up to 256 columns, whose rings hold as many bytes of W in flight as shared memory takes.
 //
-// A row's entries are sorted by column first (distill_prep_kernel), with the number of entries below each 128 columns beside
+// A row's entries are sorted by column first (distill_prep_kernel), with the number of entries below each 64 columns beside
 // them: the thread that owns the row fetches those of its columns while the tile is being multiplied.
 #pragma once
 #include <limits.h>
@@ -23,15 +25,26 @@ namespace mop {
 
 enum : int { VD_L = 0, VD_P = 1, VD_W = 2, VD_R = 3, VD_X = 4 };
 
+// VD_PAIR; VD_ONE: single CTAs, rows up to 128; VD_HALF: up to 64, whose operand takes half the room (the instruction reads 128 rows
+// all the same: what lies behind the 64 is the stage's own B, and what comes of it is not looked at).
+enum : int { VD_PAIR = 0, VD_ONE = 1, VD_HALF = 2 };
+
 // Stages, and store boxes (128 rows x 64 bf16 columns) for each column half: a tile fills two.  The router's product has a short
 // main loop (its K are the experts), so its boxes are there twice: one pair is read by the copy engine while the next is filled.
-template <int KIND>
+template <int KIND, int MODE>
 struct VdTraits {
-    static constexpr bool STORES = KIND != VD_L;
+    static constexpr bool PAIR = MODE == VD_PAIR;
+    static constexpr bool STORES = KIND != VD_L && (PAIR || KIND != VD_X);       // (a single CTA's VD_X has several ranges)
     static constexpr int SETS = KIND == VD_R ? 2 : 1;         // pairs of boxes
     static constexpr int BOXES = STORES ? 2 * SETS : 0;
-    static constexpr int STAGES = KIND == VD_L ? 6 : KIND == VD_R ? 3 : 5;
-    static constexpr int SMEM_BYTES = STAGES * T2_STAGE_BYTES + 2 * BOXES * 16384 + 1024 /*align*/ + TC_BAR_BYTES;
+    static constexpr int A_BYTES = MODE == VD_HALF ? T2_A_BYTES / 2 : T2_A_BYTES;
+    static constexpr int RING_BYTES = PAIR ? (KIND == VD_L ? 6 : KIND == VD_R ? 3 : 5) * T2_STAGE_BYTES : (STORES ? 160 : 224) * 1024;
+    static constexpr int STAGES = PAIR ? RING_BYTES / T2_STAGE_BYTES : 12;       // single CTAs: at most, as many as fit the tile's width
+    static constexpr int SMEM_BYTES = RING_BYTES + 2 * BOXES * 16384 + 1024 /*align*/ + TC_BAR_BYTES;
+    static int stages(int width) {
+        const int fit = RING_BYTES / (PAIR ? T2_STAGE_BYTES : A_BYTES + width * TC_BK * 2);
+        return fit < STAGES ? fit : STAGES;
+    }
 };
 constexpr int VD_EPI_WARPS = 8;
 constexpr int VD_THREADS = 64 + 32 * VD_EPI_WARPS;
@@ -44,6 +57,7 @@ constexpr int VD_MAX_K = 256;                                 // entries of a te
 struct VdArgs {
     int N, H, V, K;               // tokens, hidden size, vocabulary, entries per token
     int tiles_m, tiles_n, n_group, kblocks;
+    int width, stages;            // columns of a tile, stages of the ring
     int n_base;                   // VD_P: first vocabulary column of the block
     int k_base;                   // VD_X: the same, added to W's K coordinate
     int cols;                     // columns of the whole output that exist
@@ -51,17 +65,18 @@ struct VdArgs {
     int splits;                   // VD_X: ranges of K, as separate units of work (1 elsewhere)
     float c;                      // log2(e) / tau
     const int2* entry;            // [N, K] the row's entries by column (ascending): {column, place in the caller's list (VD_L) or dY (VD_P)}
-    const uint16_t* first;        // [N, units + 1] how many of them lie below column 128 u
+    const uint16_t* first;        // [N, units + 1] how many of them lie below column 64 u
     int units;
+    int parts;                    // VD_L: column ranges of `part`
     float* student;               // VD_L: [N, K] logits at the entries
-    float2* part;                 // VD_L: [N, units] (maximum, sum)
+    float2* part;                 // VD_L: [N, parts] (maximum, sum)
     const float* coef;            // VD_P: dloss / tau Q per row
     const float* lse2;            // VD_P: log-sum-exp per row in units of log 2
     const float *row_scale, *col_scale;   // VD_R: what undoes the operands' scaling, per token and per 32 columns of dX
     bf16* add_to;                 // VD_R: dX [N, cols] that the product is added to, or null
     const int32_t* seq_off;       // VD_R: offsets of the sequences or null: rows outside [seq_off[0], seq_off[n_seq]) keep what they hold
     int n_seq;
-    float* dx32;                  // VD_X: [splits, N, pitch] fp32 sums, or null: one range and one block, dX is stored at once
+    float* dx32;                  // VD_X: [splits, N, pitch] fp32 sums, or null (pairs only): one range and one block, dX is stored at once
     int pitch, accumulate;        // VD_X: add to them
     int32_t* status;
     bool gemm_follows;
@@ -80,18 +95,18 @@ __device__ __forceinline__ float ex2(float v) {
     return r;
 }
 
-// The entries of a row among 128 columns, in ascending order: the next four are in registers.
+// The entries of a row in a range of columns, in ascending order: the next four are in registers.
 struct VdEntries {
     const int2* list;
     int left;                     // entries that are not in registers yet
     int2 e[4];
-    __device__ __forceinline__ void open(const VdArgs& a, int row, int unit, bool on) {
+    __device__ __forceinline__ void open(const VdArgs& a, int row, int col, int end, bool on) {       // whole units of 64
         left = 0;
         list = a.entry;
         if (on) {
-            const uint16_t* f = a.first + (size_t)row * (a.units + 1) + unit;
-            const int from = __ldg(f);
-            left = (int)__ldg(f + 1) - from;
+            const uint16_t* f = a.first + (size_t)row * (a.units + 1);
+            const int from = __ldg(f + min(col >> 6, a.units));
+            left = (int)__ldg(f + min(end >> 6, a.units)) - from;
             list = a.entry + (size_t)row * a.K + from;
         }
 #pragma unroll
@@ -108,24 +123,49 @@ struct VdEntries {
     }
 };
 
-template <int KIND>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(VD_THREADS, 1)
+// The primitives on a pair (completing on, or signalling, both CTAs' or the leader's barriers) and on a single CTA.
+template <bool PAIR>
+__device__ __forceinline__ void vd_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+    if constexpr (PAIR) tma2_load_2d(dst, map, bar, x, y);
+    else tma_load_2d(dst, map, bar, x, y);
+}
+template <bool PAIR>
+__device__ __forceinline__ void vd_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+    if constexpr (PAIR) tma2_load_3d(dst, map, bar, x, y, z);
+    else tma_load_3d(dst, map, bar, x, y, z);
+}
+template <bool PAIR>
+__device__ __forceinline__ void vd_commit(uint32_t bar) {
+    if constexpr (PAIR) umma2_commit_both(bar);
+    else umma_commit(bar);
+}
+template <bool PAIR>
+__device__ __forceinline__ void vd_arrive(uint32_t bar) {
+    if constexpr (PAIR) mbar_arrive_pair(bar & T2_PEER_MASK);
+    else mbar_arrive(bar);
+}
+
+template <int KIND, int MODE>
+__global__ void __cluster_dims__(MODE == VD_PAIR ? 2 : 1, 1, 1) __launch_bounds__(VD_THREADS, 1)
 vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO,
                const VdArgs args) {
-    using Tr = VdTraits<KIND>;
+    using Tr = VdTraits<KIND, MODE>;
+    constexpr bool PAIR = Tr::PAIR;
+    static_assert(PAIR || KIND == VD_L || KIND == VD_P || KIND == VD_X, "the kinds whose rows are few tokens");
     constexpr int S = Tr::STAGES;
+    constexpr int TM = PAIR ? 256 : 128;
     constexpr bool A_MN = KIND == VD_W;                       // the tokens are K: X^T lies with M contiguous
     constexpr bool B_MN = KIND != VD_R && KIND != VD_X;
     extern __shared__ uint8_t tc_smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tc_smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t* boxes = smem + S * T2_STAGE_BYTES;
+    uint8_t* boxes = smem + Tr::RING_BYTES;
     uint64_t* bars = reinterpret_cast<uint64_t*>(boxes + 2 * Tr::BOXES * VD_BOX_BYTES);
     // bars: [0,S) full (leader's are used), [S,2S) empty (both), tmem_full[2] (both), tmem_empty[2] (leader's)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * S + 4);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
     const int warp = warp_index(), lane = threadIdx.x % 32;
-    const uint32_t rank = cluster_ctarank();
+    const uint32_t rank = PAIR ? cluster_ctarank() : 0u;
     const bool leader = rank == 0;
     const uint32_t smem_base = smem_u32(smem);
     const uint32_t bar_base = smem_u32(bars);
@@ -136,16 +176,19 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), 2 * VD_EPI_WARPS); }
+        for (int b = 0; b < 2; ++b) { mbar_init(tfull_bar(b), 1); mbar_init(tempty_bar(b), (PAIR ? 2 : 1) * VD_EPI_WARPS); }
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         tma_prefetch_desc(&tmA); tma_prefetch_desc(&tmB);
         if (Tr::STORES) tma_prefetch_desc(&tmO);
     }
-    if (warp == 1) tmem2_alloc(smem_u32(tmem_slot), 512);
+    if (warp == 1) {
+        if constexpr (PAIR) tmem2_alloc(smem_u32(tmem_slot), 512);
+        else tmem_alloc(smem_u32(tmem_slot), 512);
+    }
     tc_fence_before();
     __syncthreads();
-    cluster_sync_all();          // the peer's barriers exist before anything signals them
+    if constexpr (PAIR) cluster_sync_all();      // the peer's barriers exist before anything signals them
     tc_fence_after();
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
     // dX runs beside the weight gradient (of its block): both read the logit gradients, neither what the other writes.
@@ -155,7 +198,12 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     else pdl_begin_gemm(args.gemm_follows, args.note);
 
     const int tiles = args.tiles_m * args.tiles_n, total = KIND == VD_X ? tiles * args.splits : tiles;
-    const int cluster_id = blockIdx.x >> 1, n_clusters = gridDim.x >> 1;
+    const int cluster_id = PAIR ? blockIdx.x >> 1 : blockIdx.x, n_clusters = PAIR ? gridDim.x >> 1 : gridDim.x;
+    // a pair's CTAs hold half of the tile's columns each
+    const int width = PAIR && (KIND == VD_W || KIND == VD_R || KIND == VD_X) ? 256 : args.width, my_cols = PAIR ? width / 2 : width;
+    const int stages = PAIR ? S : args.stages;
+    const uint32_t stage_bytes = PAIR ? T2_STAGE_BYTES : Tr::A_BYTES + my_cols * TC_BK * 2;
+    const uint32_t copy_bytes = Tr::A_BYTES + my_cols * TC_BK * 2;
     // blocks of n_group n-tiles, row tiles slower inside one: the pairs that run at the same time cover a nearly square patch
     auto decode = [&](int t, int& mt, int& nt, int& kb0, int& kb1) {
         kb0 = 0; kb1 = args.kblocks;
@@ -178,28 +226,26 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         for (int t = cluster_id; t < total && alive; t += n_clusters) {
             int mt, nt, kb0, kb1;
             decode(t, mt, nt, kb0, kb1);
-            const int m0 = 256 * mt + 128 * (int)rank, n0 = args.n_base + 256 * nt + 128 * (int)rank;
+            const int m0 = TM * mt + 128 * (int)rank, n0 = args.n_base + width * nt + my_cols * (int)rank;
             for (int kb = kb0; kb < kb1; ++kb) {
                 if (!mbar_wait_all(empty_bar(stage), phase ^ 1u, abort_flag, args.status, STATUS_WAIT_EMPTY)) { alive = false; break; }
-                const uint32_t fb = full_bar(stage) & T2_PEER_MASK;    // the leader's barrier
-                const uint32_t sA = smem_base + stage * T2_STAGE_BYTES, sB = sA + T2_A_BYTES;
+                const uint32_t fb = PAIR ? full_bar(stage) & T2_PEER_MASK : full_bar(stage);      // the leader's barrier
+                const uint32_t sA = smem_base + stage * stage_bytes, sB = sA + Tr::A_BYTES;
                 const int k0 = kb * TC_BK;
                 if (el) {
-                    if (leader) mbar_expect_tx(full_bar(stage), 2 * T2_STAGE_BYTES);
-                    if constexpr (!A_MN) tma2_load_2d(sA, &tmA, fb, k0, m0);
-                    else if (!args.a_split) tma2_load_3d(sA, &tmA, fb, 0, k0, m0 >> 6);
+                    if (leader) mbar_expect_tx(full_bar(stage), (PAIR ? 2 : 1) * copy_bytes);
+                    if constexpr (!A_MN) vd_load_2d<PAIR>(sA, &tmA, fb, k0, m0);
+                    else if (!args.a_split) vd_load_3d<PAIR>(sA, &tmA, fb, 0, k0, m0 >> 6);
                     else {
-                        tma2_load_2d(sA, &tmA, fb, m0, k0);
-                        tma2_load_2d(sA + TC_CHUNK_BYTES, &tmA, fb, m0 + 64, k0);
+                        vd_load_2d<PAIR>(sA, &tmA, fb, m0, k0);
+                        vd_load_2d<PAIR>(sA + TC_CHUNK_BYTES, &tmA, fb, m0 + 64, k0);
                     }
-                    if constexpr (!B_MN) tma2_load_2d(sB, &tmB, fb, k0 + (KIND == VD_X ? args.k_base : 0), n0);
-                    else if (!args.b_split) tma2_load_3d(sB, &tmB, fb, 0, k0, n0 >> 6);
-                    else {
-                        tma2_load_2d(sB, &tmB, fb, n0, k0);
-                        tma2_load_2d(sB + TC_CHUNK_BYTES, &tmB, fb, n0 + 64, k0);
-                    }
+                    if constexpr (!B_MN) vd_load_2d<PAIR>(sB, &tmB, fb, k0 + (KIND == VD_X ? args.k_base : 0), n0);
+                    else if (!args.b_split) vd_load_3d<PAIR>(sB, &tmB, fb, 0, k0, n0 >> 6);
+                    else
+                        for (int q = 0; q < my_cols; q += 64) vd_load_2d<PAIR>(sB + q * (TC_CHUNK_BYTES / 64), &tmB, fb, n0 + q, k0);
                 }
-                if (++stage == S) { stage = 0; phase ^= 1u; }
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
         }
     } else if (warp == 1) {
@@ -207,7 +253,8 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         if (leader) {
             const bool el = elect_one();
             // VD_R: both operands fp16 (format 0) instead of bf16 (1)
-            constexpr uint32_t idesc = make_idesc2(A_MN, B_MN) & (KIND == VD_R ? ~((1u << 7) | (1u << 10)) : ~0u);
+            const uint32_t idesc = (((PAIR ? make_idesc2(A_MN, B_MN) : make_idesc(A_MN, B_MN)) & (KIND == VD_R ? ~((1u << 7) | (1u << 10)) : ~0u)) &
+                                    ~(63u << 17)) | ((uint32_t)(width >> 3) << 17);
             const uint64_t desc_a = A_MN ? smem_desc(0, TC_CHUNK_BYTES, 1024) : smem_desc(0, 0, 1024);
             const uint64_t desc_b = B_MN ? smem_desc(0, TC_CHUNK_BYTES, 1024) : smem_desc(0, 0, 1024);
             constexpr uint32_t a_step = (A_MN ? 2048 : 32) >> 4, b_step = (B_MN ? 2048 : 32) >> 4;
@@ -220,7 +267,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 for (int kb = kb0; kb < kb1; ++kb) {
                     if (kb == kb0 || (KIND == VD_L && kseg == VD_SEG)) {
                         if (kb > kb0) {                        // segment done: the epilogue adds it up, the next one goes to the other accumulator
-                            if (el) umma2_commit_both(tfull_bar(it & 1));
+                            if (el) vd_commit<PAIR>(tfull_bar(it & 1));
                             ++it;
                             kseg = 0;
                         }
@@ -231,20 +278,22 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                     }
                     if (!mbar_wait_all(full_bar(stage), phase, abort_flag, args.status, STATUS_WAIT_FULL)) { alive = false; break; }
                     tc_fence_after();
-                    const uint32_t sA = smem_base + stage * T2_STAGE_BYTES;
+                    const uint32_t sA = smem_base + stage * stage_bytes;
                     const uint64_t da = desc_a | (uint64_t)((sA & 0x3ffffu) >> 4);
-                    const uint64_t db = desc_b | (uint64_t)(((sA + T2_A_BYTES) & 0x3ffffu) >> 4);
+                    const uint64_t db = desc_b | (uint64_t)(((sA + Tr::A_BYTES) & 0x3ffffu) >> 4);
                     if (el) {
 #pragma unroll
-                        for (int k4 = 0; k4 < TC_BK / 16; ++k4)
-                            umma2_bf16(d_tmem, da + k4 * a_step, db + k4 * b_step, idesc, (kseg | k4) != 0 ? 1u : 0u);
-                        umma2_commit_both(empty_bar(stage));
+                        for (int k4 = 0; k4 < TC_BK / 16; ++k4) {
+                            if constexpr (PAIR) umma2_bf16(d_tmem, da + k4 * a_step, db + k4 * b_step, idesc, (kseg | k4) != 0 ? 1u : 0u);
+                            else umma_bf16(d_tmem, da + k4 * a_step, db + k4 * b_step, idesc, (kseg | k4) != 0 ? 1u : 0u);
+                        }
+                        vd_commit<PAIR>(empty_bar(stage));
                     }
                     ++kseg;
-                    if (++stage == S) { stage = 0; phase ^= 1u; }
+                    if (++stage == stages) { stage = 0; phase ^= 1u; }
                 }
                 if (!alive) break;
-                if (el) umma2_commit_both(tfull_bar(it & 1));
+                if (el) vd_commit<PAIR>(tfull_bar(it & 1));
                 ++it;
             }
         }
@@ -258,12 +307,13 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         for (int t = cluster_id; t < total && ok; t += n_clusters) {
             int mt, nt, kb0, kb1;
             decode(t, mt, nt, kb0, kb1);
-            const int row = 256 * mt + 128 * (int)rank + quarter * 32 + lane;
-            const int col0 = args.n_base + 256 * nt + 128 * half;         // vocabulary column of this thread's first
+            const int row = TM * mt + 128 * (int)rank + quarter * 32 + lane;
+            const int col0 = args.n_base + width * nt + 128 * half;       // this thread's first column of the output
+            const int tile_end = args.n_base + width * (nt + 1);          // (a half behind it has no columns)
             if constexpr (KIND == VD_L) {
                 const bool mine = row < args.N;
                 VdEntries en;
-                en.open(args, row, 2 * nt + half, mine);
+                en.open(args, row, col0, min(col0 + 128, tile_end), mine && col0 < tile_end);
                 float y[4][32];
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
@@ -283,17 +333,18 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                     }
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive_pair(tempty_bar(it & 1) & T2_PEER_MASK);
+                    if (lane == 0) vd_arrive<PAIR>(tempty_bar(it & 1));
                     ++it;
                 }
                 if (!ok) break;
                 float m = -INFINITY, sum = 0.0f;
-                if (col0 + 128 > args.cols) {             // the vocabulary ends inside these columns
+                const int end = min(args.cols, tile_end);
+                if (col0 + 128 > end) {                   // the vocabulary, or the tile, ends inside these columns
 #pragma unroll
                     for (int g = 0; g < 4; ++g)
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (col0 + 32 * g + i >= args.cols) y[g][i] = -INFINITY;
+                            if (col0 + 32 * g + i >= end) y[g][i] = -INFINITY;
                 }
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
@@ -313,7 +364,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                         args.student[(size_t)row * args.K + e.y] = v;
                     }
                 }
-                if (mine) args.part[(size_t)row * args.units + 2 * nt + half] = make_float2(m, sum);
+                if (mine && col0 < tile_end) args.part[(size_t)row * args.parts + (width > 128 ? 2 * nt + half : nt)] = make_float2(m, sum);
             } else {
                 const bool mine = row < args.N;
                 float coef = 0.0f, lse2 = 0.0f;
@@ -329,7 +380,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 VdEntries en;
                 if constexpr (KIND == VD_P) {
                     if (mine) { coef = args.coef[row]; lse2 = args.lse2[row]; }
-                    en.open(args, row, col0 >> 7, mine);
+                    en.open(args, row, col0, min(col0 + 128, tile_end), mine && col0 < tile_end);
                 }
                 bool ready = mbar_wait_warp(tfull_bar(it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, args.status, STATUS_WAIT_TMEM_FULL, lane);
                 // the four warps of a column half meet at named barriers below: they give up together or not at all
@@ -345,15 +396,15 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 tmem_ld_wait4(y[0], y[1], y[2], y[3]);
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_pair(tempty_bar(it & 1) & T2_PEER_MASK);
+                if (lane == 0) vd_arrive<PAIR>(tempty_bar(it & 1));
                 ++it;
                 if constexpr (KIND == VD_X)
-                    if (args.dx32) {                      // (whole 128-byte lines of 32 columns, a row per lane)
+                    if (!Tr::STORES || args.dx32) {                      // (whole 128-byte lines of 32 columns, a row per lane)
                         float* out = args.dx32 + ((size_t)(t / tiles) * args.N + row) * args.pitch + col0;
                         if (mine)
 #pragma unroll
                             for (int g = 0; g < 4; ++g)
-                                if (col0 + 32 * g < args.pitch) epi_f32<32>(out + 32 * g, y[g], args.accumulate);
+                                if (col0 + 32 * g < min(args.pitch, tile_end)) epi_f32<32>(out + 32 * g, y[g], args.accumulate);
                         continue;
                     }
                 const bool issuer = quarter == 0 && lane == 0;
@@ -410,10 +461,10 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
                 if (issuer) {
-                    const int x = 256 * nt + 128 * half, r0 = 256 * mt + 128 * (int)rank;
+                    const int x = width * nt + 128 * half, r0 = TM * mt + 128 * (int)rank, end = min(args.cols, width * (nt + 1));
                     if (r0 < (KIND == VD_W ? args.H : args.N)) {
-                        if (x < args.cols) tma_store_2d(&tmO, smem_u32(box), x, r0);
-                        if (x + 64 < args.cols) tma_store_2d(&tmO, smem_u32(box + VD_BOX_BYTES), x + 64, r0);
+                        if (x < end) tma_store_2d(&tmO, smem_u32(box), x, r0);
+                        if (x + 64 < end) tma_store_2d(&tmO, smem_u32(box + VD_BOX_BYTES), x + 64, r0);
                     }
                     tma_store_commit();
                 }
@@ -431,10 +482,11 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         while (clock64() - t0 < 2000000ll) __nanosleep(1000);
         __syncthreads();
     }
-    cluster_sync_all();          // neither CTA leaves while the other may still signal its barriers
+    if constexpr (PAIR) cluster_sync_all();      // neither CTA leaves while the other may still signal its barriers
     if (warp == 1) {
         tc_fence_after();
-        tmem2_dealloc(tmem_base, 512);
+        if constexpr (PAIR) tmem2_dealloc(tmem_base, 512);
+        else tmem_dealloc(tmem_base, 512);
     }
 }
 
@@ -566,47 +618,74 @@ __global__ void __launch_bounds__(32 * DP_WARPS) distill_prep_kernel(const Disti
             int lo = 0, hi = K;
             while (lo < hi) {
                 const int mid = (lo + hi) >> 1;
-                if (scols[warp][mid] < (long long)u * 128) lo = mid + 1; else hi = mid;
+                if (scols[warp][mid] < (long long)u * 64) lo = mid + 1; else hi = mid;
             }
             a.first[(size_t)n * (a.units + 1) + u] = (uint16_t)lo;
         }
     }
 }
 
-// A warp per row: lse from the row's (maximum, sum) pairs, then the loss, lanes over the entries.
+// A block per row: lse from the row's (maximum, sum) pairs, four warps over the pairs; then the loss, the first warp's lanes over the
+// entries, whose values it has fetched before.
 struct DistillMerge {
     DistillLists l;
-    const float2* part; int units;
+    const float2* part; int parts;
     const float* student;
     float c;
     float *loss, *lse;
 };
+constexpr int DM_THREADS = 128;
 template <int J>
-__global__ void __launch_bounds__(32 * DP_WARPS) distill_merge_kernel(const DistillMerge a) {
+__global__ void __launch_bounds__(DM_THREADS) distill_merge_kernel(const DistillMerge a) {
     pdl_begin();
-    const int lane = threadIdx.x % 32, K = a.l.K, n = blockIdx.x * DP_WARPS + threadIdx.x / 32;
-    if (n >= a.l.N) return;
-    const float2* row = a.part + (size_t)n * a.units;
+    __shared__ float sh[2][DM_THREADS / 32];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, K = a.l.K;
+    const size_t n = blockIdx.x;
+    const float2* row = a.part + n * a.parts;
+    constexpr int HELD = 4;                               // pairs of a thread that stay in registers
+    float2 v[HELD];
     float m = -INFINITY, t = 0.0f;
-#pragma unroll 4
-    for (int i = lane; i < a.units; i += 32) m = fmaxf(m, row[i].x);
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) {
+        v[i] = make_float2(-INFINITY, 0.0f);
+        if (threadIdx.x + i * DM_THREADS < a.parts) v[i] = row[threadIdx.x + i * DM_THREADS];
+        m = fmaxf(m, v[i].x);
+    }
+    for (int i = threadIdx.x + HELD * DM_THREADS; i < a.parts; i += DM_THREADS) m = fmaxf(m, row[i].x);
+    int32_t col[J];
+    float q[J], logq[J], s[J];
+    if (warp == 0) {
+        distill_teacher<J>(a.l, n, lane, col, q, logq);
+#pragma unroll
+        for (int j = 0; j < J; ++j) s[j] = lane + 32 * j < K ? a.student[n * K + lane + 32 * j] : 0.0f;
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) sh[0][warp] = m;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < DM_THREADS / 32; ++w) m = fmaxf(m, sh[0][w]);
     const float mc = m == -INFINITY ? 0.0f : m * a.c;
-#pragma unroll 4
-    for (int i = lane; i < a.units; i += 32) {
-        const float2 q = row[i];
-        t += q.y * exp2f(fmaf(q.x, a.c, -mc));            // (a unit behind the last column: 0 x 2^-inf)
+    // (a range behind the last column: 0 x 2^-inf)
+#pragma unroll
+    for (int i = 0; i < HELD; ++i) t += v[i].y * exp2f(fmaf(v[i].x, a.c, -mc));
+    for (int i = threadIdx.x + HELD * DM_THREADS; i < a.parts; i += DM_THREADS) {
+        const float2 p = row[i];
+        t += p.y * exp2f(fmaf(p.x, a.c, -mc));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+    if (lane == 0) sh[1][warp] = t;
+    __syncthreads();
+    if (warp != 0) return;
+    t = 0.0f;
+#pragma unroll
+    for (int w = 0; w < DM_THREADS / 32; ++w) t += sh[1][w];
     const float lse = __fdiv_rn(m, a.l.tau) + logf(t);
-    int32_t col[J];
-    float q[J], logq[J], sum = 0.0f;
-    distill_teacher<J>(a.l, n, lane, col, q, logq);
+    float sum = 0.0f;
 #pragma unroll
     for (int j = 0; j < J; ++j)
-        if (q[j] != 0.0f) sum += q[j] * (logq[j] - __fdiv_rn(a.student[(size_t)n * K + lane + 32 * j], a.l.tau) + lse);
+        if (q[j] != 0.0f) sum += q[j] * (logq[j] - __fdiv_rn(s[j], a.l.tau) + lse);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     if (lane == 0) { a.lse[n] = lse; a.loss[n] = sum; }
@@ -632,24 +711,53 @@ __global__ void __launch_bounds__(256) distill_dx_kernel(const float* __restrict
 }
 
 // ------------------------------------------------------------------------------------------ host
-template <int KIND>
+template <int KIND, int MODE>
 inline mop_status vd_set_smem() {
-    return cudaFuncSetAttribute(vd_gemm_kernel<KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, VdTraits<KIND>::SMEM_BYTES) == cudaSuccess
-               ? MOP_OK : MOP_ERR_CUDA;
+    return cudaFuncSetAttribute(vd_gemm_kernel<KIND, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                VdTraits<KIND, MODE>::SMEM_BYTES) == cudaSuccess ? MOP_OK : MOP_ERR_CUDA;
+}
+template <int KIND>
+inline mop_status vd_set_smem_rows() {
+    mop_status r;
+    if ((r = vd_set_smem<KIND, VD_PAIR>()) != MOP_OK) return r;
+    if ((r = vd_set_smem<KIND, VD_ONE>()) != MOP_OK) return r;
+    return vd_set_smem<KIND, VD_HALF>();
 }
 inline mop_status vd_init() {
     mop_status r;
-    if ((r = vd_set_smem<VD_L>()) != MOP_OK) return r;
-    if ((r = vd_set_smem<VD_P>()) != MOP_OK) return r;
-    if ((r = vd_set_smem<VD_R>()) != MOP_OK) return r;
-    if ((r = vd_set_smem<VD_X>()) != MOP_OK) return r;
-    return vd_set_smem<VD_W>();
+    if ((r = vd_set_smem_rows<VD_L>()) != MOP_OK) return r;
+    if ((r = vd_set_smem_rows<VD_P>()) != MOP_OK) return r;
+    if ((r = vd_set_smem_rows<VD_X>()) != MOP_OK) return r;
+    return vd_set_smem<VD_W, VD_PAIR>();
 }
+template <int KIND, int MODE>
+inline mop_status vd_launch(const TcPlan* p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, VdArgs args, cudaStream_t st) {
+    args.stages = VdTraits<KIND, MODE>::stages(args.width);
+    const int grid = MODE == VD_PAIR ? p->sm_count & ~1 : p->sm_count;
+    return pdl_launch(vd_gemm_kernel<KIND, MODE>, grid, VD_THREADS, VdTraits<KIND, MODE>::SMEM_BYTES, st, a, b, o, args) == cudaSuccess
+               ? MOP_OK : MOP_ERR_CUDA;
+}
+// The mode by the number of rows.
+inline int vd_mode(int N) { return N <= 64 ? VD_HALF : N <= 128 ? VD_ONE : VD_PAIR; }
+inline int vd_row_box(int mode) { return mode == VD_HALF ? 64 : 128; }      // rows of X (or dY) that a CTA copies
 template <int KIND>
-inline mop_status vd_launch(const TcPlan* p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const VdArgs& args,
-                            cudaStream_t st) {
-    return pdl_launch(vd_gemm_kernel<KIND>, p->sm_count & ~1, VD_THREADS, VdTraits<KIND>::SMEM_BYTES, st, a, b, o, args) == cudaSuccess ? MOP_OK
-                                                                                                                      : MOP_ERR_CUDA;
+inline mop_status vd_launch_rows(int mode, const TcPlan* p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const VdArgs& args,
+                                 cudaStream_t st) {
+    return mode == VD_PAIR ? vd_launch<KIND, VD_PAIR>(p, a, b, o, args, st)
+           : mode == VD_ONE ? vd_launch<KIND, VD_ONE>(p, a, b, o, args, st) : vd_launch<KIND, VD_HALF>(p, a, b, o, args, st);
+}
+constexpr int VD_SMS = 148;                   // what the rules below count with
+// Columns of a tile: the width for which the busiest CTA (or pair) has the fewest columns to do, 16 more counted for every tile's start
+// and end; wide ones where it makes no difference.  Single CTAs take any whole chunks of 64, pairs one or two of them per CTA.
+inline int vd_width(int mode, int N, int cols) {
+    const int rows = mode == VD_PAIR ? (N + 255) / 256 : 1, workers = mode == VD_PAIR ? VD_SMS / 2 : VD_SMS, step = mode == VD_PAIR ? 128 : 64;
+    int pick = 256;
+    long long best = 1ll << 60;
+    for (int w = 256; w >= step; w -= step) {
+        const long long tiles = (long long)rows * ((cols + w - 1) / w), cost = (tiles + workers - 1) / workers * (w + 16);
+        if (cost < best) { best = cost; pick = w; }
+    }
+    return pick;
 }
 // 2-D map over `cols` columns of a bf16 matrix whose rows are `pitch` elements apart, for stores; box = {64 columns, 128 rows}.
 inline bool vd_map_out(const TcPlan* p, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch) {
@@ -664,16 +772,19 @@ inline int vd_block(int N, int V) {
     const int blocks = (int)((V + most - 1) / most);
     return (int)(((long long)(V + blocks - 1) / blocks + 255) / 256 * 256);
 }
-// Ranges of K of the dX product, by the makespan of the round-robin over the pairs in microseconds: a K block of a tile takes 0.3, a
-// unit 2 more, and each range its sums' way to L2 and back.
-constexpr int VD_MAX_SPLITS = 16, VD_PAIRS = 74;
+// Ranges of K of the dX product, by the makespan of the round-robin in microseconds: a K block of a tile takes 0.3, a unit 2 more, and
+// each range its sums' way to L2 and back.
+constexpr int VD_MAX_SPLITS = 64;
 inline int vd_splits(int N, int H, int width) {
-    const int tiles = ((N + 255) / 256) * ((H + 255) / 256), kb = (width + 63) / 64;
+    const bool pair = vd_mode(N) == VD_PAIR;
+    const int workers = pair ? VD_SMS / 2 : VD_SMS;
+    const int tiles = (pair ? (N + 255) / 256 : 1) * ((H + 255) / 256), kb = (width + 63) / 64;
     const double t_sum = 8e-6 * N * H / 5.0;
-    int pick = 1;
+    int pick = 1;                             // (what is left of a single K block)
     double best = 1e30;
     for (int s = 1; s <= VD_MAX_SPLITS && s <= kb; ++s) {
-        const double t = ((tiles * (long long)s + VD_PAIRS - 1) / VD_PAIRS) * (((kb + s - 1) / s) * 0.3 + 2.0) + (s > 1 ? t_sum * s : 0.0);
+        if (s == 1 && !pair) continue;                    // (their sums go through memory anyway)
+        const double t = ((tiles * (long long)s + workers - 1) / workers) * (((kb + s - 1) / s) * 0.3 + 2.0) + (s > 1 ? t_sum * s : 0.0);
         if (t < 0.97 * best) { best = t; pick = s; }
     }
     return pick;

@@ -1316,6 +1316,7 @@ mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logi
     if (dX_opt && tensor) {
         VdArgs g{};
         g.N = s.T; g.H = s.d; g.tiles_m = ceil_div(s.T, 256); g.tiles_n = ceil_div(s.d, 256); g.n_group = g.tiles_n; g.splits = 1;
+        g.width = 256;
         g.kblocks = a.Ep / TC_BK; g.cols = s.d; g.row_scale = a.row_scale; g.col_scale = a.col_scale;
         g.add_to = accumulate ? static_cast<bf16*>(dX_opt) : nullptr; g.seq_off = seq_offsets; g.n_seq = n_seq;
         g.status = c->status; g.note = note;
@@ -1323,7 +1324,7 @@ mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logi
         if (!tc_map_2d(&c->plan, &mA, a.dz16, s.T, a.Ep, 128) || !tc_map_2d(&c->plan, &mB, a.w16, s.d, a.Ep, 128) ||
             !vd_map_out(&c->plan, &mO, dX_opt, s.T, s.d, s.d))
             return MOP_ERR_CUDA;
-        LAUNCH(c, "balance_dx", st, r = vd_launch<VD_R>(&c->plan, mA, mB, mO, g, st));
+        LAUNCH(c, "balance_dx", st, r = vd_launch<VD_R, VD_PAIR>(&c->plan, mA, mB, mO, g, st));
         if (r == MOP_OK) r = after_launch(c);
     } else if (dX_opt) {
         LAUNCH(c, "balance_dx", st,
@@ -1868,26 +1869,31 @@ mop_status mop_vocab_loss_bwd(int device, int32_t N, int32_t H, int32_t V, const
 // Distillation from a teacher's top logits through the same projection
 // ---------------------------------------------------------------------------------------------
 namespace {
-struct DistillLayout { size_t status, entry, first, coef, lse2, part, dy, dx32, total; int units, vc, blocks, splits, pitch; };
+struct DistillLayout { size_t status, entry, first, coef, lse2, part, dy, dx32, total; int mode, width, parts, units, vc, blocks, splits, pitch; bool sums; };
 DistillLayout distill_layout(int N, int H, int V, int K, bool backward) {
     DistillLayout L{};
     size_t o = 0;
     auto take = [&](size_t b) { size_t r = o; o += align_up(b); return r; };
-    L.units = 2 * ceil_div(V, 256);
+    L.units = ceil_div(V, 64);
+    L.mode = vd_mode(N);
     L.status = take(256);                 // first: mop_vocab_poll reads it without knowing the shape
     L.entry = take((size_t)N * K * 8);
     L.first = take((size_t)N * (L.units + 1) * 2);
     if (!backward) {
-        L.part = take((size_t)L.units * N * 8);
+        L.width = vd_width(L.mode, N, V);
+        L.parts = ceil_div(V, L.width) * (L.width > 128 ? 2 : 1);
+        L.part = take((size_t)L.parts * N * 8);
     } else if (N > 0) {
         L.vc = vd_block(N, V);
         L.blocks = ceil_div(V, L.vc);
+        L.width = vd_width(L.mode, N, V < L.vc ? V : L.vc);
         L.splits = vd_splits(N, H, V < L.vc ? V : L.vc);
         L.pitch = ceil_div(H, 32) * 32;   // dX is added up in whole runs of 32 columns
         L.coef = take((size_t)N * 4);
         L.lse2 = take((size_t)N * 4);
         L.dy = take((size_t)N * L.vc * 2);
-        if (L.blocks > 1 || L.splits > 1) L.dx32 = take((size_t)L.splits * N * L.pitch * 4);
+        L.sums = L.blocks > 1 || L.splits > 1 || L.mode != VD_PAIR;
+        if (L.sums) L.dx32 = take((size_t)L.splits * N * L.pitch * 4);
     }
     L.total = o;
     return L;
@@ -1900,9 +1906,9 @@ mop_status distill_check(int device, int32_t N, int32_t H, int32_t V, int32_t K,
     return MOP_OK;
 }
 bool distill_sizes_ok(int32_t N, int32_t H, int32_t V, int32_t K) { return distill_check(0, N, H, V, K, 1.0f) == MOP_OK; }
-// W_voc (or X, transposed) as an operand with its columns contiguous: 64-wide chunks, two in a copy where there are only whole ones.
-bool distill_map_mn(const TcPlan* p, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols) {
-    return tc_map_mn(p, m, base, rows, cols, 2);
+// W_voc (or X, transposed) as an operand with its columns contiguous: 64-wide chunks, a CTA's in one copy where there are only whole ones.
+bool distill_map_mn(const TcPlan* p, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, int cols_of_cta) {
+    return tc_map_mn(p, m, base, rows, cols, cols_of_cta / 64);
 }
 }  // namespace
 
@@ -1931,7 +1937,8 @@ mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, in
     const DistillLayout L = distill_layout(N, H, V, K, false);
     char* w = static_cast<char*>(workspace);
     CUtensorMap mX, mW;
-    if (!tc_map_2d(p, &mX, X, N, H, 128) || !distill_map_mn(p, &mW, W_voc, H, V)) return MOP_ERR_CUDA;
+    if (!tc_map_2d(p, &mX, X, N, H, vd_row_box(L.mode)) || !distill_map_mn(p, &mW, W_voc, H, V, L.mode == VD_PAIR ? L.width / 2 : L.width))
+        return MOP_ERR_CUDA;
     const DistillLists lists = {teacher_idx, teacher_logits, teacher_lse_opt, N, V, K, temperature};
     DistillPrep a{};
     a.l = lists; a.entry = reinterpret_cast<int2*>(w + L.entry); a.first = reinterpret_cast<uint16_t*>(w + L.first); a.units = L.units;
@@ -1943,14 +1950,15 @@ mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, in
 #undef GO
     VdArgs g{};
     g.N = N; g.H = H; g.V = V; g.K = K;
-    g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(V, 256); g.n_group = VOCAB_N_GROUP; g.kblocks = ceil_div(H, TC_BK);
+    g.width = L.width;
+    g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(V, L.width); g.n_group = VOCAB_N_GROUP; g.kblocks = ceil_div(H, TC_BK);
     g.cols = V; g.b_split = V % 64 != 0; g.c = (float)(1.4426950408889634 / temperature);
-    g.splits = 1; g.entry = a.entry; g.first = a.first; g.units = L.units; g.student = student; g.part = reinterpret_cast<float2*>(w + L.part);
+    g.splits = 1; g.entry = a.entry; g.first = a.first; g.units = L.units; g.parts = L.parts; g.student = student; g.part = reinterpret_cast<float2*>(w + L.part);
     g.status = a.status;
-    if ((r = vd_launch<VD_L>(p, mX, mW, mW, g, st)) != MOP_OK) return r;
+    if ((r = vd_launch_rows<VD_L>(L.mode, p, mX, mW, mW, g, st)) != MOP_OK) return r;
     DistillMerge m{};
-    m.l = lists; m.part = g.part; m.units = L.units; m.student = student; m.c = g.c; m.loss = loss; m.lse = lse;
-#define GO(J) pdl_launch(distill_merge_kernel<J>, ceil_div(N, DP_WARPS), 32 * DP_WARPS, 0, st, m)
+    m.l = lists; m.part = g.part; m.parts = L.parts; m.student = student; m.c = g.c; m.loss = loss; m.lse = lse;
+#define GO(J) pdl_launch(distill_merge_kernel<J>, N, DM_THREADS, 0, st, m)
     DISTILL_BY_K(K, GO);
 #undef GO
     return cudaGetLastError() == cudaSuccess ? MOP_OK : MOP_ERR_CUDA;
@@ -1981,10 +1989,12 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
     char* w = static_cast<char*>(workspace);
     int32_t* status = reinterpret_cast<int32_t*>(w + L.status);
     bf16* dY = reinterpret_cast<bf16*>(w + L.dy);
-    float* dx32 = L.blocks > 1 || L.splits > 1 ? reinterpret_cast<float*>(w + L.dx32) : nullptr;
+    float* dx32 = L.sums ? reinterpret_cast<float*>(w + L.dx32) : nullptr;
     CUtensorMap mX, mXT, mWn, mWk, mdX;
-    if (!tc_map_2d(p, &mX, X, N, H, 128) || !distill_map_mn(p, &mXT, X, N, H) || !distill_map_mn(p, &mWn, W_voc, H, V) ||
-        !tc_map_2d(p, &mWk, W_voc, H, V, 128) || !vd_map_out(p, &mdX, dX, N, H, H))
+    const int box = vd_row_box(L.mode);
+    if (!tc_map_2d(p, &mX, X, N, H, box) || !distill_map_mn(p, &mXT, X, N, H, 128) ||
+        !distill_map_mn(p, &mWn, W_voc, H, V, L.mode == VD_PAIR ? L.width / 2 : L.width) ||
+        !tc_map_2d(p, &mWk, W_voc, H, V, L.mode == VD_PAIR ? 128 : 256) || !vd_map_out(p, &mdX, dX, N, H, H))
         return MOP_ERR_CUDA;
     DistillPrep a{};
     a.l = {teacher_idx, teacher_logits, teacher_lse_opt, N, V, K, temperature};
@@ -1999,26 +2009,28 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
     for (int c0 = 0; c0 < V; c0 += L.vc) {
         const int cw = V - c0 < L.vc ? V - c0 : L.vc, cw64 = ceil_div(cw, 64) * 64;
         CUtensorMap mdYk, mdYn, mdYo, mdW;
-        if (!tc_map_2d_pitch(p, &mdYk, dY, N, cw, L.vc, 128) || !tc_map_chunked_2d_pitch(p, &mdYn, dY, N, cw64, L.vc, 2) ||
+        if (!tc_map_2d_pitch(p, &mdYk, dY, N, cw, L.vc, box) || !tc_map_chunked_2d_pitch(p, &mdYn, dY, N, cw64, L.vc, 2) ||
             !vd_map_out(p, &mdYo, dY, N, L.vc, L.vc) || !vd_map_out(p, &mdW, static_cast<bf16*>(dW_voc) + c0, H, cw, V))
             return MOP_ERR_CUDA;
         const bool last = c0 + L.vc >= V;
         VdArgs base{};
         base.N = N; base.H = H; base.V = V; base.K = K; base.n_group = VOCAB_N_GROUP; base.splits = 1; base.status = status;
+        base.width = 256;
         base.gemm_follows = true;
         const PdlNote note = {status + VOCAB_NOTE, c0 / L.vc + 1};
         {   // dY block, logits formed again on the tensor cores
             VdArgs g = base;
-            g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(cw, 256); g.kblocks = ceil_div(H, TC_BK);
+            g.width = L.width;
+            g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(cw, L.width); g.kblocks = ceil_div(H, TC_BK);
             g.n_base = c0; g.cols = cw64; g.b_split = V % 64 != 0; g.c = (float)(1.4426950408889634 / temperature);
             g.entry = a.entry; g.first = a.first; g.units = L.units; g.coef = a.coef; g.lse2 = a.lse2;
-            if ((r = vd_launch<VD_P>(p, mX, mWn, mdYo, g, st)) != MOP_OK) return r;
+            if ((r = vd_launch_rows<VD_P>(L.mode, p, mX, mWn, mdYo, g, st)) != MOP_OK) return r;
         }
         {   // dW[:, block] = X^T dY (K = the N tokens), written once
             VdArgs g = base;
             g.tiles_m = ceil_div(H, 256); g.tiles_n = ceil_div(cw, 256); g.kblocks = ceil_div(N, TC_BK);
             g.cols = cw; g.a_split = H % 64 != 0; g.note = note;
-            if ((r = vd_launch<VD_W>(p, mXT, mdYn, mdW, g, st)) != MOP_OK) return r;
+            if ((r = vd_launch<VD_W, VD_PAIR>(p, mXT, mdYn, mdW, g, st)) != MOP_OK) return r;
         }
         {   // dX (+)= dY W[:, block]^T, its CTAs take over from those of the weight gradient (as in mop_vocab_loss_bwd)
             VdArgs g = base;
@@ -2026,7 +2038,7 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
             g.splits = min(L.splits, g.kblocks);          // (the first block is the widest and writes the sums of every range)
             g.cols = H; g.dx32 = dx32; g.pitch = L.pitch; g.accumulate = c0 > 0 ? 1 : 0;
             g.note = note; g.gemm_follows = !last;        // the small blocks that follow the last one must not pile up
-            if ((r = vd_launch<VD_X>(p, mdYk, mWk, mdX, g, st)) != MOP_OK) return r;
+            if ((r = vd_launch_rows<VD_X>(L.mode, p, mdYk, mWk, mdX, g, st)) != MOP_OK) return r;
         }
     }
     if (!dx32) return MOP_OK;

@@ -86,6 +86,14 @@ SHAPES = [
     (64, 1032, 4160, 100, 1.0, True, 1.0),               # five segments of K, the last of one block that is nearly empty
     (37, 72, 1000, 256, 0.5, False, 0.1),                # the longest lists, all within 100 columns: places named many times
     (1100, 136, 520, 128, 1.0, False, 1.0),
+    # tiles of every width on single CTAs (one row per lane quarter and more), and both widths of a pair
+    (3, 64, 9472, 20, 1.0, False, 1.0),                  # 64 columns
+    (65, 128, 18944 - 8, 20, 1.0, True, 1.0),            # 128
+    (64, 264, 28416 - 64, 31, 2.0, False, 1.0),          # 192
+    (128, 128, 37888, 70, 1.0, False, 1.0),              # 256
+    (90, 72, 57000, 9, 1.0, False, 0.01),                # 192, two rounds
+    (129, 128, 9472 - 128, 40, 1.0, False, 1.0),         # a pair's 128
+    (33, 2048, 264, 12, 1.0, False, 1.0),                # few columns, a long sum
 ]
 
 

@@ -94,3 +94,38 @@ def test_workspace_sizes_need_no_device_and_take_every_shape():
     assert lib.mop_vocab_distill_fwd(0, 4, 60, 64, 2, *[None] * 5, f(1.0), *[None] * 5) == 3
     assert lib.mop_vocab_distill_bwd(0, 4, 64, 64, 257, *[None] * 5, f(1.0), *[None] * 7) == 2
     assert lib.mop_vocab_distill_bwd(99, 4, 64, 64, 2, *[None] * 5, f(1.0), *[None] * 7) == 1
+
+
+def test_tiles_stages_and_boxes_fit_shared_memory(tmp_path):
+    """Every kind in every mode: the ring, the store boxes and the barriers fit 227 KiB, a stage is whole swizzle atoms, a half-height
+    operand is followed by enough of its own stage for the 128 rows that the instruction reads; every width that the rule picks covers the
+    columns, and its entries and partial sums are counted in the same units everywhere."""
+    run_host_program(tmp_path, r"""
+#include "distill.cuh"
+#include <cstdio>
+using namespace mop;
+template <int KIND, int MODE> int check() {
+    using Tr = VdTraits<KIND, MODE>;
+    int bad = Tr::SMEM_BYTES > 232448;
+    for (int w = Tr::PAIR ? 128 : 64; w <= 256; w += Tr::PAIR ? 128 : 64) {
+        const int st = Tr::stages(w), bytes = Tr::PAIR ? T2_STAGE_BYTES : Tr::A_BYTES + w * TC_BK * 2;
+        bad += st < 3 || st > Tr::STAGES || st * bytes > Tr::RING_BYTES || bytes % 1024 || bytes < T2_A_BYTES;
+        bad += (2 * Tr::STAGES + 4) * 8 + 8 > TC_BAR_BYTES;
+    }
+    if (bad) std::printf("kind %d mode %d: %d bytes\n", KIND, MODE, Tr::SMEM_BYTES);
+    return bad;
+}
+int main() {
+    int bad = check<VD_L, VD_PAIR>() + check<VD_L, VD_ONE>() + check<VD_L, VD_HALF>() + check<VD_P, VD_PAIR>() + check<VD_P, VD_ONE>() +
+              check<VD_P, VD_HALF>() + check<VD_X, VD_PAIR>() + check<VD_X, VD_ONE>() + check<VD_X, VD_HALF>() + check<VD_W, VD_PAIR>() + check<VD_R, VD_PAIR>();
+    bool seen[5] = {};
+    for (int N : {1, 64, 65, 128, 129, 256, 257, 8192})
+        for (int V = 8; V < 200000; V += V < 1000 ? 8 : 1000) {
+            const int mode = vd_mode(N), w = vd_width(mode, N, V);
+            if (w < 64 || w > 256 || w % (mode == VD_PAIR ? 128 : 64)) { std::printf("N %d V %d: %d\n", N, V, w); ++bad; }
+            else if (mode != VD_PAIR) seen[w / 64] = true;
+            if (mode == VD_HALF ? N > 64 : mode == VD_ONE ? N > 128 : N <= 128) ++bad;
+        }
+    return bad || !(seen[1] && seen[2] && seen[3] && seen[4]);
+}
+""")
