@@ -14,8 +14,9 @@
 // a pair would multiply as much again in vain, and half of its stages would hold X: reading W is all there is then, and the product
 // runs on single CTAs, tiles of 128 rows and up to 256 columns, whose rings hold as many bytes of W in flight as shared memory takes.
 //
-// A row's entries are sorted by column first (distill_prep_kernel), with the number of entries below each 64 columns beside
-// them: the thread that owns the row fetches those of its columns while the tile is being multiplied.
+// On pairs, a row's entries are sorted by column first (distill_prep_kernel), with the number of entries below each 64 columns beside
+// them: the thread that owns the row fetches those of its columns while the tile is being multiplied.  On single CTAs a thread has
+// the same row in all its tiles and waits long for the first one: it reads the whole list itself, which saves the launch.
 #pragma once
 #include <limits.h>
 
@@ -54,6 +55,11 @@ constexpr int VD_BOX_BYTES = 128 * 64 * 2;
 constexpr int VD_SEG = 8;
 constexpr int VD_MAX_K = 256;                                 // entries of a teacher's list
 
+struct DistillLists {
+    const int32_t* idx; const float* logits; const float* lse;      // the caller's: [N,K], [N,K], [N] or null
+    int N, V, K;
+    float tau;
+};
 struct VdArgs {
     int N, H, V, K;               // tokens, hidden size, vocabulary, entries per token
     int tiles_m, tiles_n, n_group, kblocks;
@@ -70,6 +76,9 @@ struct VdArgs {
     int parts;                    // VD_L: column ranges of `part`
     float* student;               // VD_L: [N, K] logits at the entries
     float2* part;                 // VD_L: [N, parts] (maximum, sum)
+    DistillLists lists;           // single CTAs: the teacher's, and for VD_P what distill_prep_kernel reads elsewhere
+    const float *student_in, *lse, *dloss;
+    int32_t* clear;               // single CTAs, the first kernel of a call: the status block, whose words it clears
     const float* coef;            // VD_P: dloss / tau Q per row
     const float* lse2;            // VD_P: log-sum-exp per row in units of log 2
     const float *row_scale, *col_scale;   // VD_R: what undoes the operands' scaling, per token and per 32 columns of dX
@@ -145,6 +154,79 @@ __device__ __forceinline__ void vd_arrive(uint32_t bar) {
     else mbar_arrive(bar);
 }
 
+// The same without the sorted lists: the thread goes through its row's list, keeps the first four entries of its columns and goes
+// through the list again for others (`each` is called for all of them, in the list's order).
+struct VdScan {
+    const int32_t* list;
+    int K, col, end, found;
+    int2 e[4];
+    __device__ __forceinline__ void open(const DistillLists& l, int row, int from, int to, bool on) {
+        list = l.idx + (size_t)row * l.K;
+        K = on ? l.K : 0; col = from; end = min(to, l.V); found = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = make_int2(INT_MAX, 0);
+#pragma unroll 8
+        for (int k = 0; k < K; ++k) {
+            const int v = __ldg(list + k);
+            if (v < col || v >= end) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (found == i) e[i] = make_int2(v, k);
+            ++found;
+        }
+    }
+    template <class F>
+    __device__ __forceinline__ void each(F&& f) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < found) f(e[i]);
+        if (found <= 4) return;
+        int seen = 0;
+        for (int k = 0; k < K; ++k) {
+            const int v = __ldg(list + k);
+            if (v >= col && v < end && ++seen > 4) f(make_int2(v, k));
+        }
+    }
+};
+// What VD_P needs of a row (distill_prep_kernel's values), by one thread: log-sum-exp of the teacher's entries and their total probability.
+struct VdRow {
+    float g, lse, norm, total;
+    __device__ __forceinline__ static float at(const DistillLists& l, size_t i) {          // t / tau of an entry, -inf where there is none
+        const int v = __ldg(l.idx + i);
+        return v >= 0 && v < l.V ? __fdiv_rn(__ldg(l.logits + i), l.tau) : -INFINITY;
+    }
+    __device__ __forceinline__ void open(const VdArgs& a, size_t row) {
+        const DistillLists& l = a.lists;
+        g = __fdiv_rn(a.dloss[row], l.tau);
+        lse = a.lse[row];
+        float s = 0.0f;
+        if (l.lse) {
+            norm = l.lse[row];
+#pragma unroll 4
+            for (int k = 0; k < l.K; ++k) s += expf(at(l, row * l.K + k) - norm);
+            total = s;
+        } else {
+            float m = -INFINITY;
+#pragma unroll 4
+            for (int k = 0; k < l.K; ++k) m = fmaxf(m, at(l, row * l.K + k));
+            if (m == -INFINITY) m = 0.0f;
+#pragma unroll 4
+            for (int k = 0; k < l.K; ++k) s += expf(at(l, row * l.K + k) - m);
+            norm = s == 0.0f ? 0.0f : m + logf(s);
+            total = s == 0.0f ? 0.0f : s / s;             // (1, or NaN)
+        }
+    }
+    // dY of an entry: every entry of its column counts
+    __device__ __forceinline__ float dy(const VdArgs& a, size_t row, int2 e) const {
+        const DistillLists& l = a.lists;
+        float same = 0.0f;
+        for (int k = 0; k < l.K; ++k)
+            if (__ldg(l.idx + row * l.K + k) == e.x) same += expf(at(l, row * l.K + k) - norm);
+        const float p = expf(__fdiv_rn(a.student_in[row * l.K + e.y], l.tau) - lse);
+        return g * fmaf(total, p, -same);
+    }
+};
+
 template <int KIND, int MODE>
 __global__ void __cluster_dims__(MODE == VD_PAIR ? 2 : 1, 1, 1) __launch_bounds__(VD_THREADS, 1)
 vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const __grid_constant__ CUtensorMap tmO,
@@ -196,6 +278,8 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const bool beside = BESIDE && args.note.word;
     if (beside) pdl_begin_beside(args.gemm_follows, args.note);
     else pdl_begin_gemm(args.gemm_follows, args.note);
+    if constexpr (!PAIR && KIND != VD_X)
+        if (args.clear && blockIdx.x == 0 && threadIdx.x == 0) { args.clear[0] = 0; args.clear[VOCAB_NOTE] = 0; }     // (a wait runs out after seconds)
 
     const int tiles = args.tiles_m * args.tiles_n, total = KIND == VD_X ? tiles * args.splits : tiles;
     const int cluster_id = PAIR ? blockIdx.x >> 1 : blockIdx.x, n_clusters = PAIR ? gridDim.x >> 1 : gridDim.x;
@@ -304,6 +388,10 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const uint32_t ta0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * 128;
         int it = 0;
         bool ok = true;
+        VdRow of_row;
+        (void)of_row;
+        if constexpr (!PAIR && KIND == VD_P)
+            if (quarter * 32 + lane < args.N) of_row.open(args, quarter * 32 + lane);     // (the row of all its tiles)
         for (int t = cluster_id; t < total && ok; t += n_clusters) {
             int mt, nt, kb0, kb1;
             decode(t, mt, nt, kb0, kb1);
@@ -313,7 +401,10 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             if constexpr (KIND == VD_L) {
                 const bool mine = row < args.N;
                 VdEntries en;
-                en.open(args, row, col0, min(col0 + 128, tile_end), mine && col0 < tile_end);
+                VdScan scan;
+                (void)en; (void)scan;
+                if constexpr (PAIR) en.open(args, row, col0, min(col0 + 128, tile_end), mine && col0 < tile_end);
+                else scan.open(args.lists, row, col0, min(col0 + 128, tile_end), mine);
                 float y[4][32];
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
@@ -355,15 +446,25 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 for (int g = 0; g < 4; ++g) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) sum += ex2(fmaf(y[g][i], args.c, -mc));
-                    while (en.e[0].x < col0 + 32 * (g + 1)) {             // (entries lie inside the vocabulary)
-                        const int2 e = en.take();
-                        const int i = e.x - col0 - 32 * g;
+                    if constexpr (PAIR)
+                        while (en.e[0].x < col0 + 32 * (g + 1)) {         // (entries lie inside the vocabulary)
+                            const int2 e = en.take();
+                            const int i = e.x - col0 - 32 * g;
+                            float v = 0.0f;
+#pragma unroll
+                            for (int q = 0; q < 32; ++q) v = i == q ? y[g][q] : v;
+                            args.student[(size_t)row * args.K + e.y] = v;
+                        }
+                }
+                if constexpr (!PAIR)
+                    scan.each([&](int2 e) {
                         float v = 0.0f;
 #pragma unroll
-                        for (int q = 0; q < 32; ++q) v = i == q ? y[g][q] : v;
+                        for (int g = 0; g < 4; ++g)
+#pragma unroll
+                            for (int q = 0; q < 32; ++q) v = e.x - col0 == 32 * g + q ? y[g][q] : v;
                         args.student[(size_t)row * args.K + e.y] = v;
-                    }
-                }
+                    });
                 if (mine && col0 < tile_end) args.part[(size_t)row * args.parts + (width > 128 ? 2 * nt + half : nt)] = make_float2(m, sum);
             } else {
                 const bool mine = row < args.N;
@@ -378,9 +479,14 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                     if (args.add_to && args.seq_off) inside = row >= __ldg(args.seq_off) && row < __ldg(args.seq_off + args.n_seq);
                 }
                 VdEntries en;
-                if constexpr (KIND == VD_P) {
+                VdScan scan;
+                (void)en; (void)scan;
+                if constexpr (KIND == VD_P && PAIR) {
                     if (mine) { coef = args.coef[row]; lse2 = args.lse2[row]; }
                     en.open(args, row, col0, min(col0 + 128, tile_end), mine && col0 < tile_end);
+                } else if constexpr (KIND == VD_P) {
+                    if (mine) { coef = of_row.g * of_row.total; lse2 = of_row.lse * 1.4426950408889634f; }
+                    scan.open(args.lists, row, col0, min(col0 + 128, tile_end), mine);
                 }
                 bool ready = mbar_wait_warp(tfull_bar(it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, args.status, STATUS_WAIT_TMEM_FULL, lane);
                 // the four warps of a column half meet at named barriers below: they give up together or not at all
@@ -450,7 +556,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                         *reinterpret_cast<uint4*>(rowp + ((j ^ (lane & 7)) << 4)) =
                             make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
                     }
-                    if constexpr (KIND == VD_P)
+                    if constexpr (KIND == VD_P && PAIR)
                         while (en.e[0].x < col0 + 64 * (h + 1)) {         // the teacher's entries among these columns
                             const int2 e = en.take();
                             const int i = e.x - col0 - 64 * h;
@@ -458,6 +564,13 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                                 __float2bfloat16_rn(__int_as_float(e.y));
                         }
                 }
+                if constexpr (KIND == VD_P && !PAIR)
+                    scan.each([&](int2 e) {
+                        const int i = e.x - col0;
+                        uint8_t* rowp = box + (i >> 6) * VD_BOX_BYTES + (quarter * 32 + lane) * 128;
+                        *reinterpret_cast<bf16*>(rowp + ((((i & 63) >> 3) ^ (lane & 7)) << 4) + (i & 7) * 2) =
+                            __float2bfloat16_rn(of_row.dy(args, row, e));
+                    });
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
                 if (issuer) {
@@ -491,11 +604,6 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 }
 
 // ------------------------------------------------------------------------------------------ the teacher's lists
-struct DistillLists {
-    const int32_t* idx; const float* logits; const float* lse;      // the caller's: [N,K], [N,K], [N] or null
-    int N, V, K;
-    float tau;
-};
 // Teacher's probabilities of the entries lane + 32 j of row n (0 where there is none), and log q; a row without entries has none.
 template <int J>
 __device__ __forceinline__ void distill_teacher(const DistillLists& l, size_t n, int lane, int32_t (&col)[J], float (&q)[J], float (&logq)[J]) {
@@ -535,7 +643,6 @@ __device__ __forceinline__ void distill_teacher(const DistillLists& l, size_t n,
 struct DistillPrep {
     DistillLists l;
     int2* entry; uint16_t* first; int units;                        // as in VdArgs
-    float* student_out;                                             // forward: entries outside the vocabulary get 0
     const float* student; const float* lse; const float* dloss;     // backward
     float* coef; float* lse2;
     int32_t* status;
@@ -566,7 +673,6 @@ __global__ void __launch_bounds__(32 * DP_WARPS) distill_prep_kernel(const Disti
                 const int k = lane + 32 * j;
                 const int32_t v = k < K ? a.l.idx[(size_t)n * K + k] : -1;
                 col[j] = v >= 0 && v < a.l.V ? v : INT_MAX;
-                if (k < K && col[j] == INT_MAX) a.student_out[(size_t)n * K + k] = 0.0f;
             }
         }
         __syncwarp();
@@ -630,7 +736,7 @@ __global__ void __launch_bounds__(32 * DP_WARPS) distill_prep_kernel(const Disti
 struct DistillMerge {
     DistillLists l;
     const float2* part; int parts;
-    const float* student;
+    float* student;
     float c;
     float *loss, *lse;
 };
@@ -657,7 +763,12 @@ __global__ void __launch_bounds__(DM_THREADS) distill_merge_kernel(const Distill
     if (warp == 0) {
         distill_teacher<J>(a.l, n, lane, col, q, logq);
 #pragma unroll
-        for (int j = 0; j < J; ++j) s[j] = lane + 32 * j < K ? a.student[n * K + lane + 32 * j] : 0.0f;
+        for (int j = 0; j < J; ++j) {
+            s[j] = 0.0f;
+            if (lane + 32 * j >= K) continue;
+            if (col[j] != INT_MAX) s[j] = a.student[n * K + lane + 32 * j];
+            else a.student[n * K + lane + 32 * j] = 0.0f;
+        }
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));

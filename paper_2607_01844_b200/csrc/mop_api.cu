@@ -1877,8 +1877,10 @@ DistillLayout distill_layout(int N, int H, int V, int K, bool backward) {
     L.units = ceil_div(V, 64);
     L.mode = vd_mode(N);
     L.status = take(256);                 // first: mop_vocab_poll reads it without knowing the shape
-    L.entry = take((size_t)N * K * 8);
-    L.first = take((size_t)N * (L.units + 1) * 2);
+    if (L.mode == VD_PAIR) {
+        L.entry = take((size_t)N * K * 8);
+        L.first = take((size_t)N * (L.units + 1) * 2);
+    }
     if (!backward) {
         L.width = vd_width(L.mode, N, V);
         L.parts = ceil_div(V, L.width) * (L.width > 128 ? 2 : 1);
@@ -1889,8 +1891,10 @@ DistillLayout distill_layout(int N, int H, int V, int K, bool backward) {
         L.width = vd_width(L.mode, N, V < L.vc ? V : L.vc);
         L.splits = vd_splits(N, H, V < L.vc ? V : L.vc);
         L.pitch = ceil_div(H, 32) * 32;   // dX is added up in whole runs of 32 columns
-        L.coef = take((size_t)N * 4);
-        L.lse2 = take((size_t)N * 4);
+        if (L.mode == VD_PAIR) {
+            L.coef = take((size_t)N * 4);
+            L.lse2 = take((size_t)N * 4);
+        }
         L.dy = take((size_t)N * L.vc * 2);
         L.sums = L.blocks > 1 || L.splits > 1 || L.mode != VD_PAIR;
         if (L.sums) L.dx32 = take((size_t)L.splits * N * L.pitch * 4);
@@ -1942,11 +1946,10 @@ mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, in
     const DistillLists lists = {teacher_idx, teacher_logits, teacher_lse_opt, N, V, K, temperature};
     DistillPrep a{};
     a.l = lists; a.entry = reinterpret_cast<int2*>(w + L.entry); a.first = reinterpret_cast<uint16_t*>(w + L.first); a.units = L.units;
-    a.student_out = student;
     a.status = reinterpret_cast<int32_t*>(w + L.status);
     const int blocks = min(ceil_div(N, DP_WARPS), p->sm_count * 8);
 #define GO(J) pdl_launch(distill_prep_kernel<J, false>, blocks, 32 * DP_WARPS, 0, st, a)
-    DISTILL_BY_K(K, GO);
+    if (L.mode == VD_PAIR) DISTILL_BY_K(K, GO);
 #undef GO
     VdArgs g{};
     g.N = N; g.H = H; g.V = V; g.K = K;
@@ -1954,7 +1957,7 @@ mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, in
     g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(V, L.width); g.n_group = VOCAB_N_GROUP; g.kblocks = ceil_div(H, TC_BK);
     g.cols = V; g.b_split = V % 64 != 0; g.c = (float)(1.4426950408889634 / temperature);
     g.splits = 1; g.entry = a.entry; g.first = a.first; g.units = L.units; g.parts = L.parts; g.student = student; g.part = reinterpret_cast<float2*>(w + L.part);
-    g.status = a.status;
+    g.status = a.status; g.lists = lists; g.clear = a.status;
     if ((r = vd_launch_rows<VD_L>(L.mode, p, mX, mW, mW, g, st)) != MOP_OK) return r;
     DistillMerge m{};
     m.l = lists; m.part = g.part; m.parts = L.parts; m.student = student; m.c = g.c; m.loss = loss; m.lse = lse;
@@ -2004,7 +2007,7 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
     a.status = status;
     const int blocks = min(ceil_div(N, DP_WARPS), p->sm_count * 8);
 #define GO(J) pdl_launch(distill_prep_kernel<J, true>, blocks, 32 * DP_WARPS, 0, st, a)
-    DISTILL_BY_K(K, GO);
+    if (L.mode == VD_PAIR) DISTILL_BY_K(K, GO);
 #undef GO
     for (int c0 = 0; c0 < V; c0 += L.vc) {
         const int cw = V - c0 < L.vc ? V - c0 : L.vc, cw64 = ceil_div(cw, 64) * 64;
@@ -2024,6 +2027,8 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
             g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(cw, L.width); g.kblocks = ceil_div(H, TC_BK);
             g.n_base = c0; g.cols = cw64; g.b_split = V % 64 != 0; g.c = (float)(1.4426950408889634 / temperature);
             g.entry = a.entry; g.first = a.first; g.units = L.units; g.coef = a.coef; g.lse2 = a.lse2;
+            g.lists = a.l; g.student_in = student; g.lse = lse; g.dloss = dloss;
+            g.clear = c0 == 0 ? status : nullptr;
             if ((r = vd_launch_rows<VD_P>(L.mode, p, mX, mWn, mdYo, g, st)) != MOP_OK) return r;
         }
         {   // dW[:, block] = X^T dY (K = the N tokens), written once
