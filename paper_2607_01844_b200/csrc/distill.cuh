@@ -199,19 +199,26 @@ struct VdRow {
         const DistillLists& l = a.lists;
         g = __fdiv_rn(a.dloss[row], l.tau);
         lse = a.lse[row];
-        float s = 0.0f;
+        // one pass, eight entries' loads in flight: running maximum and sum (from the teacher's own log-sum-exp where there is one)
+        float m = l.lse ? l.lse[row] : -INFINITY, s = 0.0f;
+        for (int k0 = 0; k0 < l.K; k0 += 8) {
+            float v[8], top = m;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k0 + i < l.K ? at(l, row * l.K + k0 + i) : -INFINITY;
+            if (!l.lse) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i]);
+                if (top == -INFINITY) { for (int i = 0; i < 8; ++i) s += v[i] == -INFINITY ? 0.0f : v[i]; continue; }     // (NaN stays)
+                s *= expf(m - top);
+                m = top;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s += expf(v[i] - m);
+        }
         if (l.lse) {
-            norm = l.lse[row];
-#pragma unroll 4
-            for (int k = 0; k < l.K; ++k) s += expf(at(l, row * l.K + k) - norm);
+            norm = m;
             total = s;
         } else {
-            float m = -INFINITY;
-#pragma unroll 4
-            for (int k = 0; k < l.K; ++k) m = fmaxf(m, at(l, row * l.K + k));
-            if (m == -INFINITY) m = 0.0f;
-#pragma unroll 4
-            for (int k = 0; k < l.K; ++k) s += expf(at(l, row * l.K + k) - m);
             norm = s == 0.0f ? 0.0f : m + logf(s);
             total = s == 0.0f ? 0.0f : s / s;             // (1, or NaN)
         }
@@ -220,6 +227,7 @@ struct VdRow {
     __device__ __forceinline__ float dy(const VdArgs& a, size_t row, int2 e) const {
         const DistillLists& l = a.lists;
         float same = 0.0f;
+#pragma unroll 8
         for (int k = 0; k < l.K; ++k)
             if (__ldg(l.idx + row * l.K + k) == e.x) same += expf(at(l, row * l.K + k) - norm);
         const float p = expf(__fdiv_rn(a.student_in[row * l.K + e.y], l.tau) - lse);
@@ -859,13 +867,15 @@ inline mop_status vd_launch_rows(int mode, const TcPlan* p, const CUtensorMap& a
 }
 constexpr int VD_SMS = 148;                   // what the rules below count with
 // Columns of a tile: the width for which the busiest CTA (or pair) has the fewest columns to do, 16 more counted for every tile's start
-// and end; wide ones where it makes no difference.  Single CTAs take any whole chunks of 64, pairs one or two of them per CTA.
+// and end; wide ones where it makes no difference.  Single CTAs take any whole chunks of 64.  Pairs take one or two chunks per CTA; with
+// one, X's tile is as much traffic as W's (N 300, H 2048, V 32000 forward: 62 us in 4 rounds of 256 columns, 79 in 7 of 128), which
+// counts as 64 columns.
 inline int vd_width(int mode, int N, int cols) {
     const int rows = mode == VD_PAIR ? (N + 255) / 256 : 1, workers = mode == VD_PAIR ? VD_SMS / 2 : VD_SMS, step = mode == VD_PAIR ? 128 : 64;
     int pick = 256;
     long long best = 1ll << 60;
     for (int w = 256; w >= step; w -= step) {
-        const long long tiles = (long long)rows * ((cols + w - 1) / w), cost = (tiles + workers - 1) / workers * (w + 16);
+        const long long tiles = (long long)rows * ((cols + w - 1) / w), cost = (tiles + workers - 1) / workers * (w + (mode == VD_PAIR ? 64 : 16));
         if (cost < best) { best = cost; pick = w; }
     }
     return pick;
