@@ -139,15 +139,28 @@ __global__ void __launch_bounds__(512) balance_fwd_kernel(const BalFwdArgs a) {
         float acc[4 * NV];
 #pragma unroll
         for (int i = 0; i < 4 * NV; ++i) acc[i] = 0.0f;
-        for (int tb = t + warp * tpw; tb < stop; tb += W * tpw) {
+        // a row of logits, and the lane's pick, are fetched one round ahead
+        float next[4 * NV];
+        int pick = -1;
+        auto fetch = [&](int tb) {
             const int mine = tb + group;
             const bool on = mine < stop;
+            bal_load<NV>(a.logits + (size_t)mine * s.E, s, e0, on, next);
+            pick = on && in_group < s.k ? __ldg(a.idx + (size_t)mine * s.k + in_group) : -1;
+        };
+        fetch(t + warp * tpw);
+        for (int tb = t + warp * tpw; tb < stop; tb += W * tpw) {
+            const int mine = tb + group, e_pick = pick;
+            const bool on = mine < stop;
             float z[4 * NV], oms[4 * NV];
-            bal_load<NV>(a.logits + (size_t)mine * s.E, s, e0, on, z);
+#pragma unroll
+            for (int i = 0; i < 4 * NV; ++i) z[i] = next[i];
+            fetch(tb + W * tpw);
+            if (e_pick >= 0 && e_pick < s.E) atomicAdd(&cnt[e_pick], 1);   // integers: any order gives the same counts
             if (on)
-                for (int j = in_group; j < s.k; j += s.G) {
+                for (int j = in_group + s.G; j < s.k; j += s.G) {
                     const int e = a.idx[(size_t)mine * s.k + j];
-                    if (e >= 0 && e < s.E) atomicAdd(&cnt[e], 1);         // integers: any order gives the same counts
+                    if (e >= 0 && e < s.E) atomicAdd(&cnt[e], 1);
                 }
             if (a.bias)
 #pragma unroll
@@ -192,43 +205,70 @@ __global__ void __launch_bounds__(512) balance_fwd_kernel(const BalFwdArgs a) {
         __syncthreads();
         t = stop;
     }
+    if (gridDim.x > 1) return;
+    // a single block: no other kernel follows, so the sequences without tokens are its own
+    for (int seq = warp; seq < a.q.S; seq += W) {
+        if (bal_off(a.q, seq + 1) > bal_off(a.q, seq)) continue;
+        for (int e = lane; e < s.E; e += 32) { a.prob[(size_t)seq * s.E + e] = 0.0f; a.counts[(size_t)seq * s.E + e] = 0; }
+        if (lane == 0) a.loss[seq] = 0.0f;
+    }
 }
 
-// The sequences that several blocks hold a part of, and those without tokens.  Thread (slice, e) adds every slices-th block's sums.
-__global__ void __launch_bounds__(1024) balance_finish_kernel(const BalFwdArgs a) {
+// The sequences that several blocks hold a part of, and those without tokens.  Thread (slice, vector) adds every slices-th block's sums
+// of four experts (of one where the rows are no whole vectors).
+constexpr int BF_THREADS = 1024;
+__global__ void __launch_bounds__(BF_THREADS) balance_finish_kernel(const BalFwdArgs a) {
     pdl_begin();
     __shared__ float sh[32];
-    __shared__ float sp[1024];
-    __shared__ int32_t sc[1024];
-    const int E = a.s.E, Ep = (E + 31) / 32 * 32, slices = (int)blockDim.x / Ep;
-    const int e = threadIdx.x % Ep, slice = threadIdx.x / Ep;
+    __shared__ __align__(16) float sp[4 * BF_THREADS];
+    __shared__ __align__(16) int32_t sc[4 * BF_THREADS];
+    const int E = a.s.E, per = a.s.vec4 ? 4 : 1, vecs = E / per, slices = BF_THREADS / vecs;      // (E is at most 1024)
+    const int vec = threadIdx.x % vecs, slice = threadIdx.x / vecs, tid = threadIdx.x;
     for (int seq = blockIdx.x; seq < a.q.S; seq += gridDim.x) {
         const int first = bal_off(a.q, seq), last = bal_off(a.q, seq + 1);
         const int b0 = first / a.chunk, b1 = (last - 1) / a.chunk;
         if (last > first && b0 == b1) continue;                           // done by its block
-        float p = 0.0f;
-        int32_t c = 0;
-        if (last > first && slice < slices && e < E)
+        float4 p = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        int4 c = make_int4(0, 0, 0, 0);
+        if (last > first && slice < slices) {
+            if (per == 4) {
+#pragma unroll 6
+                for (int b = b0 + slice; b <= b1; b += slices) {
+                    const size_t slot = ((size_t)b * 2 + (b == b0 ? 1 : 0)) * E + 4 * vec;
+                    const float4 x = *reinterpret_cast<const float4*>(a.part_p + slot);
+                    const int4 y = *reinterpret_cast<const int4*>(a.part_c + slot);
+                    p.x += x.x; p.y += x.y; p.z += x.z; p.w += x.w;
+                    c.x += y.x; c.y += y.y; c.z += y.z; c.w += y.w;
+                }
+            } else {
 #pragma unroll 8
-            for (int b = b0 + slice; b <= b1; b += slices) {
-                const size_t slot = ((size_t)b * 2 + (b == b0 ? 1 : 0)) * E + e;
-                p += a.part_p[slot];
-                c += a.part_c[slot];
+                for (int b = b0 + slice; b <= b1; b += slices) {
+                    const size_t slot = ((size_t)b * 2 + (b == b0 ? 1 : 0)) * E + vec;
+                    p.x += a.part_p[slot];
+                    c.x += a.part_c[slot];
+                }
             }
-        sp[threadIdx.x] = p;
-        sc[threadIdx.x] = c;
+        }
+        if (slice < slices) {
+            if (per == 4) {
+                *reinterpret_cast<float4*>(sp + 4 * tid) = p;
+                *reinterpret_cast<int4*>(sc + 4 * tid) = c;
+            } else { sp[tid] = p.x; sc[tid] = c.x; }
+        }
         __syncthreads();
         float dot = 0.0f;
         const float n = (float)max(1, last - first);
-        if (slice == 0 && e < E) {
-            for (int i = 1; i < slices; ++i) { p += sp[i * Ep + e]; c += sc[i * Ep + e]; }
-            p /= n;
-            a.prob[(size_t)seq * E + e] = p;
-            a.counts[(size_t)seq * E + e] = c;
-            dot = (float)c * p;
+        if (tid < E) {                                                    // slice i holds its sums E further on
+            float q = 0.0f;
+            int32_t d = 0;
+            for (int i = 0; i < slices; ++i) { q += sp[i * E + tid]; d += sc[i * E + tid]; }
+            q /= n;
+            a.prob[(size_t)seq * E + tid] = q;
+            a.counts[(size_t)seq * E + tid] = d;
+            dot = (float)d * q;
         }
         dot = bal_block_sum(dot, sh);
-        if (threadIdx.x == 0) a.loss[seq] = dot * ((float)E / ((float)a.s.k * n));
+        if (tid == 0) a.loss[seq] = dot * ((float)E / ((float)a.s.k * n));
         __syncthreads();
     }
 }
@@ -305,8 +345,8 @@ __device__ __forceinline__ void bal_copy_edge(const BalBwdArgs& a, int edge, int
 // dz, zero for tokens outside the sequences.  Counts are taken relative to their mean (k T_s / E, rounded): c_e - sum p c does not
 // change by a shift, and under a nearly balanced load, which this loss aims at, the difference keeps its digits.
 // The blocks behind the first dz_blocks prepare W_r and the edges of x.
-template <int NV>
-__global__ void __launch_bounds__(256) balance_dz_kernel(const BalBwdArgs a) {
+template <int NV, bool PRE>
+__global__ void __launch_bounds__(256, NV <= 2 ? 3 : 1) balance_dz_kernel(const BalBwdArgs a) {
     pdl_begin();
     extern __shared__ float bal_smem[];                                   // [W][E]
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.note = 0;
@@ -323,13 +363,14 @@ __global__ void __launch_bounds__(256) balance_dz_kernel(const BalBwdArgs a) {
     const int W = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int tpw = 32 / s.G, in_group = lane % s.G, group = lane / s.G, e0 = 4 * in_group;
     const int c0 = blockIdx.x * a.chunk, c1 = min(s.T, c0 + a.chunk);
-    float bias[4 * NV], acc[4 * NV];
+    float bias[PRE ? 4 * NV : 1], acc[PRE ? 4 * NV : 1];
+    if constexpr (PRE)
 #pragma unroll
-    for (int i = 0; i < 4 * NV; ++i) {
-        const int e = e0 + 4 * s.G * (i / 4) + i % 4;
-        bias[i] = a.bias && e < s.E ? a.bias[e] : 0.0f;
-        acc[i] = 0.0f;
-    }
+        for (int i = 0; i < 4 * NV; ++i) {
+            const int e = e0 + 4 * s.G * (i / 4) + i % 4;
+            bias[i] = e < s.E ? a.bias[e] : 0.0f;
+            acc[i] = 0.0f;
+        }
     // the lane's sequence, and what follows from it, as long as its tokens stay inside
     int first = 0, last = 0;
     float w = 0.0f, c[4 * NV], next[4 * NV];
@@ -362,7 +403,7 @@ __global__ void __launch_bounds__(256) balance_dz_kernel(const BalBwdArgs a) {
         if (!on)
 #pragma unroll
             for (int i = 0; i < 4 * NV; ++i) z[i] = -INFINITY;            // (a padding token's logits may be anything)
-        if (a.bias)
+        if constexpr (PRE)
 #pragma unroll
             for (int i = 0; i < 4 * NV; ++i) z[i] += bias[i];
         bal_scores<NV>(s, z, oms);
@@ -376,7 +417,7 @@ __global__ void __launch_bounds__(256) balance_dz_kernel(const BalBwdArgs a) {
             if (s.score_fn != 0) v *= oms[i];
             const bool there = on && e0 + 4 * s.G * (i / 4) + i % 4 < s.E;
             z[i] = there ? v : 0.0f;
-            acc[i] += z[i];
+            if constexpr (PRE) acc[i] += z[i];
             amax = fmaxf(amax, fabsf(z[i]));
         }
         if (a.dz && t < c1)
@@ -418,21 +459,23 @@ __global__ void __launch_bounds__(256) balance_dz_kernel(const BalBwdArgs a) {
                 }
             }
     }
-    if (!a.dbias_part) return;
-    for (int o = s.G; o < 32; o <<= 1)
+    if constexpr (PRE) {
+        if (!a.dbias_part) return;
+        for (int o = s.G; o < 32; o <<= 1)
 #pragma unroll
-        for (int i = 0; i < 4 * NV; ++i) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], o);
-    if (group == 0)
+            for (int i = 0; i < 4 * NV; ++i) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], o);
+        if (group == 0)
 #pragma unroll
-        for (int i = 0; i < 4 * NV; ++i) {
-            const int e = e0 + 4 * s.G * (i / 4) + i % 4;
-            if (e < s.E) bal_smem[(size_t)warp * s.E + e] = acc[i];
+            for (int i = 0; i < 4 * NV; ++i) {
+                const int e = e0 + 4 * s.G * (i / 4) + i % 4;
+                if (e < s.E) bal_smem[(size_t)warp * s.E + e] = acc[i];
+            }
+        __syncthreads();
+        for (int e = threadIdx.x; e < s.E; e += blockDim.x) {
+            float v = 0.0f;
+            for (int i = 0; i < W; ++i) v += bal_smem[(size_t)i * s.E + e];
+            a.dbias_part[(size_t)blockIdx.x * s.E + e] = v;
         }
-    __syncthreads();
-    for (int e = threadIdx.x; e < s.E; e += blockDim.x) {
-        float v = 0.0f;
-        for (int i = 0; i < W; ++i) v += bal_smem[(size_t)i * s.E + e];
-        a.dbias_part[(size_t)blockIdx.x * s.E + e] = v;
     }
 }
 
@@ -840,16 +883,20 @@ __global__ void __launch_bounds__(256) balance_dx_kernel(const float* __restrict
 
 // ------------------------------------------------------------------------------------------ host
 constexpr int BAL_PAIRS = 74;             // CTA pairs that the rules below count with (148 SMs)
-// Tokens per block: one block for each SM, at least 16 tokens each.
-inline int bal_chunk(int T) { const int c = (T + 147) / 148; return c < 16 ? 16 : c; }
-inline int bal_blocks(int T) { return (T + bal_chunk(T) - 1) / bal_chunk(T); }
+inline int bal_warps(int E) { return E <= 512 ? 16 : 8; }
+// Tokens per block of the forward: a single block where six rounds of its warps do (a second launch costs more), else two blocks for
+// each SM, a round each at least.
+inline int bal_chunk(int T, int E) {
+    const int round = bal_warps(E) * (32 / bal_group(E)), c = (T + 295) / 296;
+    return T <= 6 * round ? (T > 0 ? T : 1) : c < round ? round : c;
+}
+inline int bal_blocks(int T, int E) { return (T + bal_chunk(T, E) - 1) / bal_chunk(T, E); }
 // ... of the backward: eight warps, one round of tokens for each of about 600 blocks.
 inline int bal_chunk_bwd(int T, int E) {
     const int round = 8 * (E <= 64 ? 2 : 1), c = (T + 591) / 592;
     return c < round ? round : c;
 }
 inline int bal_blocks_bwd(int T, int E) { return (T + bal_chunk_bwd(T, E) - 1) / bal_chunk_bwd(T, E); }
-inline int bal_warps(int E) { return E <= 512 ? 16 : 8; }
 inline size_t bal_smem_bytes(int E, int warps) { return (size_t)(warps + 1) * E * 4; }
 inline BalShape bal_shape(const mop_moe_shape& s) {
     return {s.T, s.E, s.k, bal_group(s.E), s.score_fn, s.E % 4 == 0};

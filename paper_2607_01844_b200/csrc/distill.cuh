@@ -7,8 +7,8 @@
 // vd_gemm_kernel runs the products, with eight epilogue warps behind a TMA producer and an MMA issuer:
 //   VD_L  Y = X W_voc: per row and up to 128 columns the maximum and the sum of exponentials, and the logits of the teacher's entries
 //   VD_P  dY, one block of vocabulary columns, bf16 (the only piece of the N x V matrix that ever exists)
-//   VD_W  dW_voc[:, block] = X^T dY, bf16
-//   VD_X  dX = dY W_voc^T, beside VD_W: the block's columns (its K) in `splits` ranges, fp32 sums over the blocks
+//   VD_X  dX = dY W_voc^T: the block's columns (its K) in `splits` ranges, fp32 sums over the blocks
+//   VD_W  dW_voc[:, block] = X^T dY, bf16, beside VD_X
 //   VD_R  the router's dX (+)= dz W_r^T (balance.cuh) from fp16 operands that are scaled by powers of two, bf16
 // With many rows on CTA pairs (256 x 256 tiles, tcgen05.mma.cta_group::2, stages of 64 of K, as tc_gemm2_kernel).  With up to 128 rows
 // a pair would multiply as much again in vain, and half of its stages would hold X: reading W is all there is then, and the product
@@ -281,8 +281,9 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     if constexpr (PAIR) cluster_sync_all();      // the peer's barriers exist before anything signals them
     tc_fence_after();
     const uint32_t tmem_base = __shfl_sync(0xffffffffu, *tmem_slot, 0);
-    // dX runs beside the weight gradient (of its block): both read the logit gradients, neither what the other writes.
-    constexpr bool BESIDE = KIND == VD_X || KIND == VD_R;
+    // The weight gradient runs beside dX of its block, the router's dX beside its weight gradient: both read the logit gradients, neither
+    // what the other writes.
+    constexpr bool BESIDE = KIND == VD_W || KIND == VD_R;
     const bool beside = BESIDE && args.note.word;
     if (beside) pdl_begin_beside(args.gemm_follows, args.note);
     else pdl_begin_gemm(args.gemm_follows, args.note);
@@ -885,9 +886,11 @@ inline bool vd_map_out(const TcPlan* p, CUtensorMap* m, const void* base, uint64
     return tc_map_2d_pitch(p, m, base, rows, cols, pitch, 128);
 }
 
-// Vocabulary columns whose logit gradients are live at a time: as many as keep dY at 2^26 elements (128 MiB), at least 8192, in blocks
-// of about equal width.  Wide blocks mean few launches, long sums and few passes over the fp32 sums of dX.
-constexpr long long VD_LIVE = 1ll << 26;
+// Vocabulary columns whose logit gradients are live at a time: as many as keep dY at 2^28 elements (512 MiB), at least 8192, in blocks
+// of about equal width.  Wide blocks mean few launches, long sums and few passes over the fp32 sums of dX.  Backward in us, blocks of up to
+// 8192, 16384, 32768, 65536 columns and all: N 1537, H 2048, V 50304 930, 829, 770, 722, 723; N 4096, H 7168, V 131072 18150, 17900,
+// 17500, 17350, 18500; N 8192 36300, 36550, 37200, 37200, 39500; N 256, H 2048, V 32000 243 in four and 123 in one.
+constexpr long long VD_LIVE = 1ll << 28;
 inline int vd_block(int N, int V) {
     const long long most = VD_LIVE / N > 8192 ? VD_LIVE / N : 8192;
     const int blocks = (int)((V + most - 1) / most);

@@ -1163,7 +1163,7 @@ BalanceLayout balance_layout(const mop_moe_shape& s, bool backward) {
     BalanceLayout L{};
     size_t o = 0;
     auto take = [&](size_t b) { size_t r = o; o += align_up(b); return r; };
-    const size_t blocks = bal_blocks(s.T), T = s.T, d = s.d, E = s.E, Ep = bal_ep(s.E);
+    const size_t blocks = bal_blocks(s.T, s.E), T = s.T, d = s.d, E = s.E, Ep = bal_ep(s.E);
     if (!backward) {
         L.part_p = take(2 * blocks * E * 4);
         L.part_c = take(2 * blocks * E * 4);
@@ -1216,16 +1216,17 @@ mop_status mop_moe_balance_loss_fwd(mop_ctx* c, int32_t n_seq, const float* logi
     char* w = static_cast<char*>(workspace);
     BalFwdArgs a{};
     a.logits = logits; a.bias = s.bias_mode == MOP_BIAS_PRE_LOGIT ? bias : nullptr; a.idx = topk_idx;
-    a.q = {seq_offsets, n_seq, s.T}; a.s = bal_shape(s); a.chunk = bal_chunk(s.T);
+    a.q = {seq_offsets, n_seq, s.T}; a.s = bal_shape(s); a.chunk = bal_chunk(s.T, s.E);
     a.counts = counts; a.prob = prob; a.loss = loss;
     a.part_p = reinterpret_cast<float*>(w + L.part_p); a.part_c = reinterpret_cast<int32_t*>(w + L.part_c);
     const int warps = bal_warps(s.E);
-#define GO(NV) pdl_launch(balance_fwd_kernel<NV>, bal_blocks(s.T), 32 * warps, bal_smem_bytes(s.E, warps), st, a)
+    const int blocks = bal_blocks(s.T, s.E);
+#define GO(NV) pdl_launch(balance_fwd_kernel<NV>, blocks, 32 * warps, bal_smem_bytes(s.E, warps), st, a)
     LAUNCH(c, "balance_fwd", st, BAL_BY_WIDTH(s.E, GO));
 #undef GO
     mop_status r = after_launch(c);
-    if (r != MOP_OK) return r;
-    LAUNCH(c, "balance_finish", st, pdl_launch(balance_finish_kernel, min(n_seq, 1184), 1024, 0, st, a));
+    if (r != MOP_OK || blocks == 1) return r;
+    LAUNCH(c, "balance_finish", st, pdl_launch(balance_finish_kernel, min(n_seq, 1184), BF_THREADS, 0, st, a));
     return after_launch(c);
 }
 
@@ -1280,7 +1281,9 @@ mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logi
             extra += min(ceil_div(s.d, 32), 2 * c->sm_count);
         }
     } else if (!a.dz && (dW_r_opt || dX_opt)) a.dz = reinterpret_cast<float*>(w + L.dz);
-#define GO(NV) pdl_launch(balance_dz_kernel<NV>, a.dz_blocks + extra, 32 * warps, bal_smem_bytes(s.E, warps), st, a)
+#define GO(NV)                                                                                                             \
+    if (pre) pdl_launch(balance_dz_kernel<NV, true>, a.dz_blocks + extra, 32 * warps, bal_smem_bytes(s.E, warps), st, a); \
+    else pdl_launch(balance_dz_kernel<NV, false>, a.dz_blocks + extra, 32 * warps, 0, st, a)
     LAUNCH(c, "balance_dz", st, BAL_BY_WIDTH(s.E, GO));
 #undef GO
     mop_status r = after_launch(c);
@@ -2031,19 +2034,20 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
             g.clear = c0 == 0 ? status : nullptr;
             if ((r = vd_launch_rows<VD_P>(L.mode, p, mX, mWn, mdYo, g, st)) != MOP_OK) return r;
         }
-        {   // dW[:, block] = X^T dY (K = the N tokens), written once
-            VdArgs g = base;
-            g.tiles_m = ceil_div(H, 256); g.tiles_n = ceil_div(cw, 256); g.kblocks = ceil_div(N, TC_BK);
-            g.cols = cw; g.a_split = H % 64 != 0; g.note = note;
-            if ((r = vd_launch<VD_W, VD_PAIR>(p, mXT, mdYn, mdW, g, st)) != MOP_OK) return r;
-        }
-        {   // dX (+)= dY W[:, block]^T, its CTAs take over from those of the weight gradient (as in mop_vocab_loss_bwd)
+        {   // dX (+)= dY W[:, block]^T, while the block's W is in L2
             VdArgs g = base;
             g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(H, 256); g.kblocks = ceil_div(cw, TC_BK); g.k_base = c0;
             g.splits = min(L.splits, g.kblocks);          // (the first block is the widest and writes the sums of every range)
             g.cols = H; g.dx32 = dx32; g.pitch = L.pitch; g.accumulate = c0 > 0 ? 1 : 0;
-            g.note = note; g.gemm_follows = !last;        // the small blocks that follow the last one must not pile up
+            g.note = note;
             if ((r = vd_launch_rows<VD_X>(L.mode, p, mdYk, mWk, mdX, g, st)) != MOP_OK) return r;
+        }
+        {   // dW[:, block] = X^T dY (K = the N tokens), written once; its CTAs take over from those of dX (as in mop_vocab_loss_bwd)
+            VdArgs g = base;
+            g.tiles_m = ceil_div(H, 256); g.tiles_n = ceil_div(cw, 256); g.kblocks = ceil_div(N, TC_BK);
+            g.cols = cw; g.a_split = H % 64 != 0; g.note = note;
+            g.gemm_follows = !last;                       // the small blocks that follow the last one must not pile up
+            if ((r = vd_launch<VD_W, VD_PAIR>(p, mXT, mdYn, mdW, g, st)) != MOP_OK) return r;
         }
     }
     if (!dx32) return MOP_OK;

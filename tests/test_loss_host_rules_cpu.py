@@ -44,7 +44,7 @@ int main() {
 
 
 def test_column_blocks_cover_the_vocabulary_in_whole_tiles(tmp_path):
-    """Blocks of the logit gradients: whole tiles (256 columns), at most 2^26 elements or 8192 columns, none of them empty, and the
+    """Blocks of the logit gradients: whole tiles (256 columns), at most 2^28 elements or 8192 columns, none of them empty, and the
     ranges of the dX product never more than the widest block's K blocks."""
     run_host_program(tmp_path, r"""
 #include "distill.cuh"
