@@ -14,9 +14,9 @@
 // a pair would multiply as much again in vain, and half of its stages would hold X: reading W is all there is then, and the product
 // runs on single CTAs, tiles of 128 rows and up to 256 columns, whose rings hold as many bytes of W in flight as shared memory takes.
 //
-// On pairs, a row's entries are sorted by column first (distill_prep_kernel), with the number of entries below each 64 columns beside
-// them: the thread that owns the row fetches those of its columns while the tile is being multiplied.  On single CTAs a thread has
-// the same row in all its tiles and waits long for the first one: it reads the whole list itself, which saves the launch.
+// A row's entries are sorted by column first (distill_prep_kernel), with the number of entries below each 64 columns beside them: the
+// thread that owns the row fetches those of its columns while the tile is being multiplied.  VD_L on single CTAs waits long for its first
+// tile: its warps read through the lists themselves, which saves the launch.
 #pragma once
 #include <limits.h>
 
@@ -76,9 +76,8 @@ struct VdArgs {
     int parts;                    // VD_L: column ranges of `part`
     float* student;               // VD_L: [N, K] logits at the entries
     float2* part;                 // VD_L: [N, parts] (maximum, sum)
-    DistillLists lists;           // single CTAs: the teacher's, and for VD_P what distill_prep_kernel reads elsewhere
-    const float *student_in, *lse, *dloss;
-    int32_t* clear;               // single CTAs, the first kernel of a call: the status block, whose words it clears
+    DistillLists lists;           // VD_L on single CTAs, the first kernel of its call: the teacher's lists, and the status block, whose
+    int32_t* clear;               // words it clears
     const float* coef;            // VD_P: dloss / tau Q per row
     const float* lse2;            // VD_P: log-sum-exp per row in units of log 2
     const float *row_scale, *col_scale;   // VD_R: what undoes the operands' scaling, per token and per 32 columns of dX
@@ -154,84 +153,61 @@ __device__ __forceinline__ void vd_arrive(uint32_t bar) {
     else mbar_arrive(bar);
 }
 
-// The same without the sorted lists: the thread goes through its row's list, keeps the first four entries of its columns and goes
-// through the list again for others (`each` is called for all of them, in the list's order).
+// The same without the sorted lists: a warp goes through the lists of its 32 rows, lanes over the entries, sixteen loads in flight, and
+// the thread that owns a row keeps the first eight entries of its columns (its offset, 7 bits, and its place in the list, 8 bits).
+// Others are looked for again when they are wanted.
 struct VdScan {
     const int32_t* list;
     int K, col, end, found;
-    int2 e[4];
-    __device__ __forceinline__ void open(const DistillLists& l, int row, int from, int to, bool on) {
-        list = l.idx + (size_t)row * l.K;
-        K = on ? l.K : 0; col = from; end = min(to, l.V); found = 0;
+    uint32_t e[4];
+    __device__ __forceinline__ void open(const DistillLists& l, int row0, int rows, int from, int to, int lane) {
+        K = l.K; col = from; end = min(to, l.V); found = 0;
+        list = l.idx + (size_t)(row0 + lane) * K;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) e[i] = make_int2(INT_MAX, 0);
-#pragma unroll 8
-        for (int k = 0; k < K; ++k) {
-            const int v = __ldg(list + k);
-            if (v < col || v >= end) continue;
+        for (int i = 0; i < 4; ++i) e[i] = 0;
+        const int words = (K + 31) / 32, n = rows * words;                // word w of row r: its entries 32 w + lane
+        const int32_t* base = l.idx + (size_t)row0 * K;
+        int r = 0, w = 0, rr = 0, ww = 0;                                 // of the next load, and of the next word that is looked at
+        for (int i0 = 0; i0 < n; i0 += 16) {
+            int v[16];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (found == i) e[i] = make_int2(v, k);
-            ++found;
-        }
-    }
-    template <class F>
-    __device__ __forceinline__ void each(F&& f) const {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < found) f(e[i]);
-        if (found <= 4) return;
-        int seen = 0;
-        for (int k = 0; k < K; ++k) {
-            const int v = __ldg(list + k);
-            if (v >= col && v < end && ++seen > 4) f(make_int2(v, k));
-        }
-    }
-};
-// What VD_P needs of a row (distill_prep_kernel's values), by one thread: log-sum-exp of the teacher's entries and their total probability.
-struct VdRow {
-    float g, lse, norm, total;
-    __device__ __forceinline__ static float at(const DistillLists& l, size_t i) {          // t / tau of an entry, -inf where there is none
-        const int v = __ldg(l.idx + i);
-        return v >= 0 && v < l.V ? __fdiv_rn(__ldg(l.logits + i), l.tau) : -INFINITY;
-    }
-    __device__ __forceinline__ void open(const VdArgs& a, size_t row) {
-        const DistillLists& l = a.lists;
-        g = __fdiv_rn(a.dloss[row], l.tau);
-        lse = a.lse[row];
-        // one pass, eight entries' loads in flight: running maximum and sum (from the teacher's own log-sum-exp where there is one)
-        float m = l.lse ? l.lse[row] : -INFINITY, s = 0.0f;
-        for (int k0 = 0; k0 < l.K; k0 += 8) {
-            float v[8], top = m;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = k0 + i < l.K ? at(l, row * l.K + k0 + i) : -INFINITY;
-            if (!l.lse) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top = fmaxf(top, v[i]);
-                if (top == -INFINITY) { for (int i = 0; i < 8; ++i) s += v[i] == -INFINITY ? 0.0f : v[i]; continue; }     // (NaN stays)
-                s *= expf(m - top);
-                m = top;
+            for (int i = 0; i < 16; ++i) {
+                v[i] = i0 + i < n && 32 * w + lane < K ? __ldg(base + (size_t)r * K + 32 * w + lane) : -1;
+                if (++w == words) { w = 0; ++r; }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s += expf(v[i] - m);
-        }
-        if (l.lse) {
-            norm = m;
-            total = s;
-        } else {
-            norm = s == 0.0f ? 0.0f : m + logf(s);
-            total = s == 0.0f ? 0.0f : s / s;             // (1, or NaN)
+            for (int i = 0; i < 16; ++i) {
+                uint32_t hits = __ballot_sync(0xffffffffu, v[i] >= col && v[i] < end);
+                while (hits) {
+                    const int b = __ffs(hits) - 1;
+                    hits &= hits - 1;
+                    const int c = __shfl_sync(0xffffffffu, v[i], b);
+                    if (lane != rr) continue;
+                    const uint32_t packed = (uint32_t)(c - col) | (uint32_t)(32 * ww + b) << 7;
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (found == q) e[q / 2] |= packed << 16 * (q % 2);
+                    ++found;
+                }
+                if (++ww == words) { ww = 0; ++rr; }
+            }
         }
     }
-    // dY of an entry: every entry of its column counts
-    __device__ __forceinline__ float dy(const VdArgs& a, size_t row, int2 e) const {
-        const DistillLists& l = a.lists;
-        float same = 0.0f;
-#pragma unroll 8
-        for (int k = 0; k < l.K; ++k)
-            if (__ldg(l.idx + row * l.K + k) == e.x) same += expf(at(l, row * l.K + k) - norm);
-        const float p = expf(__fdiv_rn(a.student_in[row * l.K + e.y], l.tau) - lse);
-        return g * fmaf(total, p, -same);
+    template <class F>            // f(offset of the column, place in the list)
+    __device__ __forceinline__ void each(F&& f) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < found) f((int)(e[i / 2] >> 16 * (i % 2) & 127u), (int)(e[i / 2] >> (16 * (i % 2) + 7) & 255u));
+        if (found <= 8) return;
+        int seen = 0;
+        for (int k0 = 0; k0 < K; k0 += 8) {
+            int v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = k0 + i < K ? __ldg(list + k0 + i) : -1;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (v[i] >= col && v[i] < end && ++seen > 8) f(v[i] - col, k0 + i);
+        }
     }
 };
 
@@ -287,7 +263,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
     const bool beside = BESIDE && args.note.word;
     if (beside) pdl_begin_beside(args.gemm_follows, args.note);
     else pdl_begin_gemm(args.gemm_follows, args.note);
-    if constexpr (!PAIR && KIND != VD_X)
+    if constexpr (!PAIR && KIND == VD_L)
         if (args.clear && blockIdx.x == 0 && threadIdx.x == 0) { args.clear[0] = 0; args.clear[VOCAB_NOTE] = 0; }     // (a wait runs out after seconds)
 
     const int tiles = args.tiles_m * args.tiles_n, total = KIND == VD_X ? tiles * args.splits : tiles;
@@ -397,10 +373,6 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
         const uint32_t ta0 = tmem_base + ((uint32_t)(quarter * 32) << 16) + half * 128;
         int it = 0;
         bool ok = true;
-        VdRow of_row;
-        (void)of_row;
-        if constexpr (!PAIR && KIND == VD_P)
-            if (quarter * 32 + lane < args.N) of_row.open(args, quarter * 32 + lane);     // (the row of all its tiles)
         for (int t = cluster_id; t < total && ok; t += n_clusters) {
             int mt, nt, kb0, kb1;
             decode(t, mt, nt, kb0, kb1);
@@ -413,7 +385,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 VdScan scan;
                 (void)en; (void)scan;
                 if constexpr (PAIR) en.open(args, row, col0, min(col0 + 128, tile_end), mine && col0 < tile_end);
-                else scan.open(args.lists, row, col0, min(col0 + 128, tile_end), mine);
+                else scan.open(args.lists, quarter * 32, min(32, max(0, args.N - quarter * 32)), col0, min(col0 + 128, tile_end), lane);
                 float y[4][32];
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
@@ -466,13 +438,13 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                         }
                 }
                 if constexpr (!PAIR)
-                    scan.each([&](int2 e) {
+                    scan.each([&](int at, int k) {
                         float v = 0.0f;
 #pragma unroll
                         for (int g = 0; g < 4; ++g)
 #pragma unroll
-                            for (int q = 0; q < 32; ++q) v = e.x - col0 == 32 * g + q ? y[g][q] : v;
-                        args.student[(size_t)row * args.K + e.y] = v;
+                            for (int q = 0; q < 32; ++q) v = at == 32 * g + q ? y[g][q] : v;
+                        args.student[(size_t)row * args.K + k] = v;
                     });
                 if (mine && col0 < tile_end) args.part[(size_t)row * args.parts + (width > 128 ? 2 * nt + half : nt)] = make_float2(m, sum);
             } else {
@@ -488,14 +460,10 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                     if (args.add_to && args.seq_off) inside = row >= __ldg(args.seq_off) && row < __ldg(args.seq_off + args.n_seq);
                 }
                 VdEntries en;
-                VdScan scan;
-                (void)en; (void)scan;
-                if constexpr (KIND == VD_P && PAIR) {
+                (void)en;
+                if constexpr (KIND == VD_P) {
                     if (mine) { coef = args.coef[row]; lse2 = args.lse2[row]; }
                     en.open(args, row, col0, min(col0 + 128, tile_end), mine && col0 < tile_end);
-                } else if constexpr (KIND == VD_P) {
-                    if (mine) { coef = of_row.g * of_row.total; lse2 = of_row.lse * 1.4426950408889634f; }
-                    scan.open(args.lists, row, col0, min(col0 + 128, tile_end), mine);
                 }
                 bool ready = mbar_wait_warp(tfull_bar(it & 1), (uint32_t)(it >> 1) & 1u, abort_flag, args.status, STATUS_WAIT_TMEM_FULL, lane);
                 // the four warps of a column half meet at named barriers below: they give up together or not at all
@@ -565,7 +533,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                         *reinterpret_cast<uint4*>(rowp + ((j ^ (lane & 7)) << 4)) =
                             make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
                     }
-                    if constexpr (KIND == VD_P && PAIR)
+                    if constexpr (KIND == VD_P)
                         while (en.e[0].x < col0 + 64 * (h + 1)) {         // the teacher's entries among these columns
                             const int2 e = en.take();
                             const int i = e.x - col0 - 64 * h;
@@ -573,13 +541,6 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                                 __float2bfloat16_rn(__int_as_float(e.y));
                         }
                 }
-                if constexpr (KIND == VD_P && !PAIR)
-                    scan.each([&](int2 e) {
-                        const int i = e.x - col0;
-                        uint8_t* rowp = box + (i >> 6) * VD_BOX_BYTES + (quarter * 32 + lane) * 128;
-                        *reinterpret_cast<bf16*>(rowp + ((((i & 63) >> 3) ^ (lane & 7)) << 4) + (i & 7) * 2) =
-                            __float2bfloat16_rn(of_row.dy(args, row, e));
-                    });
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
                 if (issuer) {
@@ -657,25 +618,32 @@ struct DistillPrep {
     int32_t* status;
 };
 constexpr int DP_WARPS = 8;
-// A warp per row: places every entry by counting the smaller ones (equal columns by their place).  Backward: dY of each entry, the
-// probabilities of equal columns added up, so that every one of them holds the same value.
+// A warp per row: sorts the entries by column (equal columns by their place in the list; those outside the vocabulary last) in registers,
+// entry 32 j + lane with lane, a bitonic network.  Backward: dY of each entry, the probabilities of equal columns added up, so that
+// every one of them holds the same value.
 template <int J, bool BWD>
 __global__ void __launch_bounds__(32 * DP_WARPS) distill_prep_kernel(const DistillPrep a) {
     pdl_begin();
-    __shared__ int32_t scols[DP_WARPS][VD_MAX_K];
-    __shared__ float sq[DP_WARPS][BWD ? VD_MAX_K : 1];
+    __shared__ int32_t scols[DP_WARPS][32 * J];
+    __shared__ float sq[DP_WARPS][BWD ? 32 * J : 1], sorted_q[DP_WARPS][BWD ? 32 * J : 1];
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, N = a.l.N, K = a.l.K;
     if (blockIdx.x == 0 && threadIdx.x == 0) { *a.status = 0; a.status[VOCAB_NOTE] = 0; }
     for (int n = blockIdx.x * DP_WARPS + warp; n < N; n += gridDim.x * DP_WARPS) {
         int32_t col[J];
         float q[J], logq[J];
-        float total = 0.0f;
+        float total = 0.0f, g = 0.0f, lse = 0.0f;
         if constexpr (BWD) {
+            g = __fdiv_rn(a.dloss[n], a.l.tau);
+            lse = a.lse[n];
             distill_teacher<J>(a.l, n, lane, col, q, logq);
 #pragma unroll
             for (int j = 0; j < J; ++j) total += q[j];
 #pragma unroll
             for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+            if (lane == 0) { a.coef[n] = g * total; a.lse2[n] = lse * 1.4426950408889634f; }
+            __syncwarp();
+#pragma unroll
+            for (int j = 0; j < J; ++j) sq[warp][lane + 32 * j] = q[j];
         } else {
 #pragma unroll
             for (int j = 0; j < J; ++j) {
@@ -684,64 +652,63 @@ __global__ void __launch_bounds__(32 * DP_WARPS) distill_prep_kernel(const Disti
                 col[j] = v >= 0 && v < a.l.V ? v : INT_MAX;
             }
         }
-        __syncwarp();
+        unsigned long long key[J];
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int k = lane + 32 * j;
-            if (k < K) { scols[warp][k] = col[j]; if constexpr (BWD) sq[warp][k] = q[j]; }
-        }
-        __syncwarp();
-        int rank[J];
-        float same[J];
+        for (int j = 0; j < J; ++j) key[j] = (unsigned long long)(uint32_t)col[j] << 8 | (uint32_t)(lane + 32 * j);
 #pragma unroll
-        for (int j = 0; j < J; ++j) { rank[j] = 0; same[j] = 0.0f; }
-        for (int i = 0; i < K; ++i) {
-            const int32_t v = scols[warp][i];
-            float w = 0.0f;
-            if constexpr (BWD) w = sq[warp][i];
+        for (int size = 2; size <= 32 * J; size *= 2)
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const int k = lane + 32 * j;
-                rank[j] += v < col[j] || (v == col[j] && i < k) ? 1 : 0;
-                if constexpr (BWD) same[j] += v == col[j] ? w : 0.0f;
-            }
-        }
-        float g = 0.0f, lse = 0.0f;
-        if constexpr (BWD) {
-            g = __fdiv_rn(a.dloss[n], a.l.tau);
-            lse = a.lse[n];
-            if (lane == 0) { a.coef[n] = g * total; a.lse2[n] = lse * 1.4426950408889634f; }
-        }
+            for (int step = size / 2; step > 0; step /= 2)
 #pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int k = lane + 32 * j;
-            if (k >= K) continue;
-            int2 e = make_int2(col[j], k);
-            if constexpr (BWD)
-                if (col[j] != INT_MAX) {
-                    const float p = expf(__fdiv_rn(a.student[(size_t)n * K + k], a.l.tau) - lse);
-                    e.y = __float_as_int(g * fmaf(total, p, -same[j]));
+                for (int j = 0; j < J; ++j) {
+                    const bool up = ((lane + 32 * j) & size) == 0;        // this run ascends
+                    if (step >= 32) {
+                        const int o = j ^ (step / 32);
+                        if (o > j && (key[j] > key[o]) == up) { const unsigned long long t = key[j]; key[j] = key[o]; key[o] = t; }
+                    } else {
+                        const unsigned long long other = __shfl_xor_sync(0xffffffffu, key[j], step);
+                        const bool low = (lane & step) == 0;
+                        if ((key[j] > other) == (up == low)) key[j] = other;
+                    }
                 }
-            a.entry[(size_t)n * K + rank[j]] = e;
-        }
-        __syncwarp();                                     // everybody has read the columns: now in order
-#pragma unroll
-        for (int j = 0; j < J; ++j)
-            if (lane + 32 * j < K) scols[warp][rank[j]] = col[j];
         __syncwarp();
-        for (int u = lane; u <= a.units; u += 32) {
-            int lo = 0, hi = K;
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (scols[warp][mid] < (long long)u * 64) lo = mid + 1; else hi = mid;
-            }
-            a.first[(size_t)n * (a.units + 1) + u] = (uint16_t)lo;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int32_t c = (int32_t)(key[j] >> 8);
+            scols[warp][lane + 32 * j] = c;
+            if constexpr (BWD) sorted_q[warp][lane + 32 * j] = sq[warp][key[j] & 255];
         }
+        __syncwarp();
+        int valid = 0;
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int at = lane + 32 * j, k = (int)(key[j] & 255);
+            const int32_t c = (int32_t)(key[j] >> 8);
+            valid += __popc(__ballot_sync(0xffffffffu, c != INT_MAX));
+            if (at >= K) continue;
+            int2 e = make_int2(c, k);
+            if (c != INT_MAX) {
+                if constexpr (BWD) {
+                    int from = at;
+                    while (from > 0 && scols[warp][from - 1] == c) --from;
+                    float same = 0.0f;
+                    for (; from < 32 * J && scols[warp][from] == c; ++from) same += sorted_q[warp][from];
+                    const float p = expf(__fdiv_rn(a.student[(size_t)n * K + k], a.l.tau) - lse);
+                    e.y = __float_as_int(g * fmaf(total, p, -same));
+                }
+                // the columns' units up to this entry's, from the one behind the entry before it
+                for (int u = at > 0 ? (scols[warp][at - 1] >> 6) + 1 : 0; u <= c >> 6; ++u)
+                    a.first[(size_t)n * (a.units + 1) + u] = (uint16_t)at;
+            }
+            a.entry[(size_t)n * K + at] = e;
+        }
+        for (int u = (valid > 0 ? (scols[warp][valid - 1] >> 6) + 1 : 0) + lane; u <= a.units; u += 32)
+            a.first[(size_t)n * (a.units + 1) + u] = (uint16_t)valid;
     }
 }
 
-// A block per row: lse from the row's (maximum, sum) pairs, four warps over the pairs; then the loss, the first warp's lanes over the
-// entries, whose values it has fetched before.
+// lse of a row from its (maximum, sum) pairs, R warps over the pairs; then the loss, the first warp's lanes over the entries, whose
+// values it has fetched before.  Four warps a row where there are few rows or long ones, else one.
 struct DistillMerge {
     DistillLists l;
     const float2* part; int parts;
@@ -750,23 +717,24 @@ struct DistillMerge {
     float *loss, *lse;
 };
 constexpr int DM_THREADS = 128;
-template <int J>
+template <int J, int R>
 __global__ void __launch_bounds__(DM_THREADS) distill_merge_kernel(const DistillMerge a) {
     pdl_begin();
-    __shared__ float sh[2][DM_THREADS / 32];
-    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, K = a.l.K;
-    const size_t n = blockIdx.x;
+    __shared__ float sh[2][R];
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32 % R, tid = warp * 32 + lane, K = a.l.K;
+    const size_t n = R == 1 ? (size_t)blockIdx.x * (DM_THREADS / 32) + threadIdx.x / 32 : blockIdx.x;
+    if (n >= a.l.N) return;                               // (whole warps, and with R > 1 no block has any)
     const float2* row = a.part + n * a.parts;
-    constexpr int HELD = 4;                               // pairs of a thread that stay in registers
+    constexpr int HELD = R == 1 ? 8 : 4;                  // pairs of a thread that stay in registers
     float2 v[HELD];
     float m = -INFINITY, t = 0.0f;
 #pragma unroll
     for (int i = 0; i < HELD; ++i) {
         v[i] = make_float2(-INFINITY, 0.0f);
-        if (threadIdx.x + i * DM_THREADS < a.parts) v[i] = row[threadIdx.x + i * DM_THREADS];
+        if (tid + i * 32 * R < a.parts) v[i] = row[tid + i * 32 * R];
         m = fmaxf(m, v[i].x);
     }
-    for (int i = threadIdx.x + HELD * DM_THREADS; i < a.parts; i += DM_THREADS) m = fmaxf(m, row[i].x);
+    for (int i = tid + HELD * 32 * R; i < a.parts; i += 32 * R) m = fmaxf(m, row[i].x);
     int32_t col[J];
     float q[J], logq[J], s[J];
     if (warp == 0) {
@@ -781,26 +749,30 @@ __global__ void __launch_bounds__(DM_THREADS) distill_merge_kernel(const Distill
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (lane == 0) sh[0][warp] = m;
-    __syncthreads();
+    if constexpr (R > 1) {
+        if (lane == 0) sh[0][warp] = m;
+        __syncthreads();
 #pragma unroll
-    for (int w = 0; w < DM_THREADS / 32; ++w) m = fmaxf(m, sh[0][w]);
+        for (int w = 0; w < R; ++w) m = fmaxf(m, sh[0][w]);
+    }
     const float mc = m == -INFINITY ? 0.0f : m * a.c;
     // (a range behind the last column: 0 x 2^-inf)
 #pragma unroll
     for (int i = 0; i < HELD; ++i) t += v[i].y * exp2f(fmaf(v[i].x, a.c, -mc));
-    for (int i = threadIdx.x + HELD * DM_THREADS; i < a.parts; i += DM_THREADS) {
+    for (int i = tid + HELD * 32 * R; i < a.parts; i += 32 * R) {
         const float2 p = row[i];
         t += p.y * exp2f(fmaf(p.x, a.c, -mc));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
-    if (lane == 0) sh[1][warp] = t;
-    __syncthreads();
-    if (warp != 0) return;
-    t = 0.0f;
+    if constexpr (R > 1) {
+        if (lane == 0) sh[1][warp] = t;
+        __syncthreads();
+        if (warp != 0) return;
+        t = 0.0f;
 #pragma unroll
-    for (int w = 0; w < DM_THREADS / 32; ++w) t += sh[1][w];
+        for (int w = 0; w < R; ++w) t += sh[1][w];
+    }
     const float lse = __fdiv_rn(m, a.l.tau) + logf(t);
     float sum = 0.0f;
 #pragma unroll
@@ -811,22 +783,27 @@ __global__ void __launch_bounds__(DM_THREADS) distill_merge_kernel(const Distill
     if (lane == 0) { a.lse[n] = lse; a.loss[n] = sum; }
 }
 
-// dX from its fp32 sums [splits, N, pitch], added in order, 8 elements a thread.
+// dX from its fp32 sums [splits, N, pitch], four elements a thread; with many ranges (few tokens, hence few elements) four lanes share
+// them, each adds every fourth range, and their sums are added in order (N 4, H 576, 64 ranges: 22 us by single threads, 7 by four).
 __global__ void __launch_bounds__(256) distill_dx_kernel(const float* __restrict__ src, bf16* __restrict__ dst, int N, int H, int pitch,
                                                          int splits) {
     pdl_begin();
-    const int per = H / 8;
-    const size_t n8 = (size_t)N * per;
-    for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < n8; i += (size_t)gridDim.x * blockDim.x) {
-        const size_t r = i / per, c = (i - r * per) * 8;
-        float v[8] = {};
-#pragma unroll 4
-        for (int s = 0; s < splits; ++s) {
-            const float4* p = reinterpret_cast<const float4*>(src + ((size_t)s * N + r) * pitch + c);
-            const float4 a = p[0], b = p[1];
-            v[0] += a.x; v[1] += a.y; v[2] += a.z; v[3] += a.w; v[4] += b.x; v[5] += b.y; v[6] += b.z; v[7] += b.w;
+    const int per = H / 4, lanes = splits >= 8 ? 4 : 1, sub = threadIdx.x % lanes, elements = 256 / lanes;
+    const size_t n4 = (size_t)N * per, step = (size_t)gridDim.x * elements;
+    for (size_t i0 = (size_t)blockIdx.x * elements; i0 < n4; i0 += step) {
+        const size_t i = i0 + threadIdx.x / lanes, r = i / per, c = (i - r * per) * 4;
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (i < n4)
+#pragma unroll 8
+            for (int s = sub; s < splits; s += lanes) {
+                const float4 p = *reinterpret_cast<const float4*>(src + ((size_t)s * N + r) * pitch + c);
+                v.x += p.x; v.y += p.y; v.z += p.z; v.w += p.w;
+            }
+        for (int o = 1; o < lanes; o *= 2) {
+            v.x += __shfl_xor_sync(0xffffffffu, v.x, o); v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+            v.z += __shfl_xor_sync(0xffffffffu, v.z, o); v.w += __shfl_xor_sync(0xffffffffu, v.w, o);
         }
-        store_bf16_run<8>(dst + r * H + c, v);
+        if (sub == 0 && i < n4) *reinterpret_cast<uint2*>(dst + r * H + c) = make_uint2(pack_bf16x2(v.x, v.y), pack_bf16x2(v.z, v.w));
     }
 }
 
@@ -867,16 +844,18 @@ inline mop_status vd_launch_rows(int mode, const TcPlan* p, const CUtensorMap& a
            : mode == VD_ONE ? vd_launch<KIND, VD_ONE>(p, a, b, o, args, st) : vd_launch<KIND, VD_HALF>(p, a, b, o, args, st);
 }
 constexpr int VD_SMS = 148;                   // what the rules below count with
-// Columns of a tile: the width for which the busiest CTA (or pair) has the fewest columns to do, 16 more counted for every tile's start
-// and end; wide ones where it makes no difference.  Single CTAs take any whole chunks of 64.  Pairs take one or two chunks per CTA; with
-// one, X's tile is as much traffic as W's (N 300, H 2048, V 32000 forward: 62 us in 4 rounds of 256 columns, 79 in 7 of 128), which
-// counts as 64 columns.
+// Columns of a tile: the width for which the busiest CTA (or pair) is done first; wide ones where it makes no difference.
+// Pairs take one or two chunks of 64 per CTA; with one, X's tile is as much traffic as W's, which counts as 64 columns (N 300, H 2048,
+// V 32000 forward: 62 us in 4 rounds of 256 columns, 79 in 7 of 128).  On single CTAs a K block costs about as much whatever the width,
+// which counts as 320 columns (forward in us, widths 64, 128, 192 and 256: N 64, H 2048, V 32000 57, 36, 40, 29; N 19, H 3008, V 44608 84,
+// 61, 52, 58; N 100, H 2048, V 50304 108, 63, 52, 54; N 16, H 4096, V 64000 138, 104, 99, 88; N 100, H 2048, V 8192, not in L2, 25, 25, 27, 29).
 inline int vd_width(int mode, int N, int cols) {
-    const int rows = mode == VD_PAIR ? (N + 255) / 256 : 1, workers = mode == VD_PAIR ? VD_SMS / 2 : VD_SMS, step = mode == VD_PAIR ? 128 : 64;
+    const bool pair = mode == VD_PAIR;
+    const int rows = pair ? (N + 255) / 256 : 1, workers = pair ? VD_SMS / 2 : VD_SMS;
     int pick = 256;
     long long best = 1ll << 60;
-    for (int w = 256; w >= step; w -= step) {
-        const long long tiles = (long long)rows * ((cols + w - 1) / w), cost = (tiles + workers - 1) / workers * (w + (mode == VD_PAIR ? 64 : 16));
+    for (int w = 256; w >= 128; w -= pair ? 128 : 64) {
+        const long long tiles = (long long)rows * ((cols + w - 1) / w), cost = (tiles + workers - 1) / workers * (w + (pair ? 64 : 320));
         if (cost < best) { best = cost; pick = w; }
     }
     return pick;

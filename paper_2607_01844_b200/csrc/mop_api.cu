@@ -1880,7 +1880,7 @@ DistillLayout distill_layout(int N, int H, int V, int K, bool backward) {
     L.units = ceil_div(V, 64);
     L.mode = vd_mode(N);
     L.status = take(256);                 // first: mop_vocab_poll reads it without knowing the shape
-    if (L.mode == VD_PAIR) {
+    if (backward || L.mode == VD_PAIR) {
         L.entry = take((size_t)N * K * 8);
         L.first = take((size_t)N * (L.units + 1) * 2);
     }
@@ -1894,10 +1894,8 @@ DistillLayout distill_layout(int N, int H, int V, int K, bool backward) {
         L.width = vd_width(L.mode, N, V < L.vc ? V : L.vc);
         L.splits = vd_splits(N, H, V < L.vc ? V : L.vc);
         L.pitch = ceil_div(H, 32) * 32;   // dX is added up in whole runs of 32 columns
-        if (L.mode == VD_PAIR) {
-            L.coef = take((size_t)N * 4);
-            L.lse2 = take((size_t)N * 4);
-        }
+        L.coef = take((size_t)N * 4);
+        L.lse2 = take((size_t)N * 4);
         L.dy = take((size_t)N * L.vc * 2);
         L.sums = L.blocks > 1 || L.splits > 1 || L.mode != VD_PAIR;
         if (L.sums) L.dx32 = take((size_t)L.splits * N * L.pitch * 4);
@@ -1964,7 +1962,10 @@ mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, in
     if ((r = vd_launch_rows<VD_L>(L.mode, p, mX, mW, mW, g, st)) != MOP_OK) return r;
     DistillMerge m{};
     m.l = lists; m.part = g.part; m.parts = L.parts; m.student = student; m.c = g.c; m.loss = loss; m.lse = lse;
-#define GO(J) pdl_launch(distill_merge_kernel<J>, N, DM_THREADS, 0, st, m)
+    const bool narrow = N >= 2048 && L.parts <= 512;      // a warp per row keeps the SMs busy
+#define GO(J)                                                                                                           \
+    if (narrow) pdl_launch(distill_merge_kernel<J, 1>, ceil_div(N, DM_THREADS / 32), DM_THREADS, 0, st, m);             \
+    else pdl_launch(distill_merge_kernel<J, 4>, N, DM_THREADS, 0, st, m)
     DISTILL_BY_K(K, GO);
 #undef GO
     return cudaGetLastError() == cudaSuccess ? MOP_OK : MOP_ERR_CUDA;
@@ -2010,7 +2011,7 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
     a.status = status;
     const int blocks = min(ceil_div(N, DP_WARPS), p->sm_count * 8);
 #define GO(J) pdl_launch(distill_prep_kernel<J, true>, blocks, 32 * DP_WARPS, 0, st, a)
-    if (L.mode == VD_PAIR) DISTILL_BY_K(K, GO);
+    DISTILL_BY_K(K, GO);
 #undef GO
     for (int c0 = 0; c0 < V; c0 += L.vc) {
         const int cw = V - c0 < L.vc ? V - c0 : L.vc, cw64 = ceil_div(cw, 64) * 64;
@@ -2030,8 +2031,6 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
             g.tiles_m = ceil_div(N, 256); g.tiles_n = ceil_div(cw, L.width); g.kblocks = ceil_div(H, TC_BK);
             g.n_base = c0; g.cols = cw64; g.b_split = V % 64 != 0; g.c = (float)(1.4426950408889634 / temperature);
             g.entry = a.entry; g.first = a.first; g.units = L.units; g.coef = a.coef; g.lse2 = a.lse2;
-            g.lists = a.l; g.student_in = student; g.lse = lse; g.dloss = dloss;
-            g.clear = c0 == 0 ? status : nullptr;
             if ((r = vd_launch_rows<VD_P>(L.mode, p, mX, mWn, mdYo, g, st)) != MOP_OK) return r;
         }
         {   // dX (+)= dY W[:, block]^T, while the block's W is in L2
@@ -2051,8 +2050,8 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
         }
     }
     if (!dx32) return MOP_OK;
-    const size_t n8 = (size_t)N * (H / 8), cap = (size_t)p->sm_count * 16;
-    pdl_launch(distill_dx_kernel, (unsigned)((n8 + 255) / 256 < cap ? (n8 + 255) / 256 : cap), 256, 0, st, dx32, static_cast<bf16*>(dX), N,
+    const size_t blocks_dx = ((size_t)N * (H / 4) + 63) / 64, cap = (size_t)p->sm_count * 16;
+    pdl_launch(distill_dx_kernel, (unsigned)(blocks_dx < cap ? blocks_dx : cap), 256, 0, st, dx32, static_cast<bf16*>(dX), N,
                H, L.pitch, L.splits);
     return cudaGetLastError() == cudaSuccess ? MOP_OK : MOP_ERR_CUDA;
 }
