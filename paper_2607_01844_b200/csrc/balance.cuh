@@ -310,6 +310,7 @@ __device__ __forceinline__ void bal_convert_w(const BalBwdArgs& a, int block, in
     for (int r0 = block * 32; r0 < a.d; r0 += blocks * 32) {
         float amax = 0.0f, up, down;
         for (int r = r0 + warp; r < min(r0 + 32, a.d); r += warps)
+#pragma unroll 4
             for (int e = lane; e < E; e += 32) amax = fmaxf(amax, fabsf(a.W_r[(size_t)r * E + e]));
         for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
         __syncthreads();
@@ -346,7 +347,7 @@ __device__ __forceinline__ void bal_copy_edge(const BalBwdArgs& a, int edge, int
 // change by a shift, and under a nearly balanced load, which this loss aims at, the difference keeps its digits.
 // The blocks behind the first dz_blocks prepare W_r and the edges of x.
 template <int NV, bool PRE>
-__global__ void __launch_bounds__(256, NV <= 2 ? 3 : 1) balance_dz_kernel(const BalBwdArgs a) {
+__global__ void __launch_bounds__(256, NV <= 2 ? 3 : NV == 4 ? 2 : 1) balance_dz_kernel(const BalBwdArgs a) {
     pdl_begin();
     extern __shared__ float bal_smem[];                                   // [W][E]
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.note = 0;
@@ -489,7 +490,7 @@ __global__ void __launch_bounds__(256, NV <= 2 ? 3 : 1) balance_dz_kernel(const 
 // T 16384, d 7168, E 256: 28 tiles of 256 blocks are 97 blocks for each pair (five equal ranges per tile made 104, and 140 sums).
 constexpr int BW_SA = 3, BW_SB = 9, BW_SLOT = 16384, BW_SEG = 3, BW_EPI_WARPS = 8;
 constexpr int BW_THREADS = 64 + 32 * BW_EPI_WARPS;
-constexpr int BW_SMEM_BYTES = (BW_SA + BW_SB) * BW_SLOT + 1024 /*align*/ + TC_BAR_BYTES;
+constexpr int BW_SMEM_BYTES = (BW_SA + BW_SB) * BW_SLOT + BW_EPI_WARPS * ROW_STAGE_BYTES + 1024 /*align*/ + TC_BAR_BYTES;
 // The row of token blocks in units of half a block of 256 experts (a last tile of at most 128 experts costs half): the tiles of 256
 // experts, row tiles fastest, then the narrow ones.
 struct BalCut {
@@ -529,7 +530,7 @@ bal_dw_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
                    const __grid_constant__ CUtensorMap tmP1, const BalDwArgs args) {
     extern __shared__ uint8_t tc_smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(tc_smem_raw) + 1023) & ~uintptr_t(1023));
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (BW_SA + BW_SB) * BW_SLOT);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + (BW_SA + BW_SB) * BW_SLOT + BW_EPI_WARPS * ROW_STAGE_BYTES);
     // bars: fullA[SA] (leader's are used), emptyA[SA] (both), fullB[SB] (leader's), emptyB[SB] (both),
     //       tmem_full[2] (both), tmem_empty[2] (leader's)
     constexpr int NBARS = 2 * BW_SA + 2 * BW_SB + 4;
@@ -711,35 +712,20 @@ bal_dw_pair_kernel(const __grid_constant__ CUtensorMap tmX, const __grid_constan
                 ++it;
             }
             if (!ok) break;
-            const int row = u.mt * 256 + 128 * (int)rank + quarter * 32 + lane;
-            if (!active || row >= args.d) continue;
+            const int row0 = u.mt * 256 + 128 * (int)rank + quarter * 32, col = u.nt * 256 + half * 128;
+            if (!active || row0 >= args.d) continue;
             const bool whole = cut.first_pair(u.tile) == cut.last_pair(u.tile);
-            const int col = u.nt * 256 + half * 128;
-            if (!whole) {                        // (rows of 256 columns, whatever the number of experts)
-                float* out = args.part + ((size_t)pair * 2 + (cut.first_pair(u.tile) < pair ? 0 : 1)) * 65536 +
-                             (size_t)(128 * (int)rank + quarter * 32 + lane) * 256 + half * 128;
+            float* sh = reinterpret_cast<float*>(smem + (BW_SA + BW_SB) * BW_SLOT) + (warp - 2) * (ROW_STAGE_BYTES / 4);
+            // (sums of a cut tile: rows of 256 columns, whatever the number of experts)
+            float* out = whole ? args.dW + (size_t)row0 * args.E + col
+                               : args.part + ((size_t)pair * 2 + (cut.first_pair(u.tile) < pair ? 0 : 1)) * 65536 +
+                                     (size_t)(128 * (int)rank + quarter * 32) * 256 + half * 128;
+            const size_t pitch = whole ? args.E : 256;
+            const bool add = whole && args.accumulate;
 #pragma unroll
-                for (int g = 0; g < 4; ++g) epi_f32<32>(out + 32 * g, sum[g], 0);
-            } else if (args.E % 4 == 0) {
-                float* out = args.dW + (size_t)row * args.E + col;
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        if (col + 32 * g + i >= args.E) continue;
-                        float4 v = make_float4(sum[g][i], sum[g][i + 1], sum[g][i + 2], sum[g][i + 3]);
-                        float4* o = reinterpret_cast<float4*>(out + 32 * g + i);
-                        if (args.accumulate) { v.x += o->x; v.y += o->y; v.z += o->z; v.w += o->w; }
-                        *o = v;
-                    }
-            } else {
-                float* out = args.dW + (size_t)row * args.E + col;
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (col + 32 * g + i < args.E) out[32 * g + i] = args.accumulate ? out[32 * g + i] + sum[g][i] : sum[g][i];
-            }
+            for (int g = 0; g < 4; ++g)
+                if (col + 32 * g < args.E)
+                    store_rows_32(sh, sum[g], out + 32 * g, pitch, min(32, args.d - row0), min(32, args.E - col - 32 * g), add, lane);
         }
     }
 

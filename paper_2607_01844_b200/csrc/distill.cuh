@@ -26,6 +26,23 @@ namespace mop {
 
 enum : int { VD_L = 0, VD_P = 1, VD_W = 2, VD_R = 3, VD_X = 4 };
 
+// 32 rows, a lane each, of 32 fp32 columns to global memory: through shared memory (rows of 33), so that a warp's store is a row's 128
+// bytes instead of 32 rows' 16 (a 256 x 256 tile's stores: about 4 us of the load-store unit's time with rows by lane, 0.6 this way).
+constexpr int ROW_STAGE_BYTES = 32 * 33 * 4;
+__device__ __forceinline__ void store_rows_32(float* sh, const float (&v)[32], float* out, size_t pitch, int rows, int cols, bool add, int lane) {
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sh[lane * 33 + i] = v[i];
+    __syncwarp();
+    if (lane >= cols) return;
+#pragma unroll 8
+    for (int r = 0; r < rows; ++r) {
+        float* o = out + r * pitch + lane;
+        const float x = sh[r * 33 + lane];
+        *o = add ? *o + x : x;
+    }
+}
+
 // VD_PAIR; VD_ONE: single CTAs, rows up to 128; VD_HALF: up to 64, whose operand takes half the room (the instruction reads 128 rows
 // all the same: what lies behind the 64 is the stage's own B, and what comes of it is not looked at).
 enum : int { VD_PAIR = 0, VD_ONE = 1, VD_HALF = 2 };
@@ -39,7 +56,8 @@ struct VdTraits {
     static constexpr int SETS = KIND == VD_R ? 2 : 1;         // pairs of boxes
     static constexpr int BOXES = STORES ? 2 * SETS : 0;
     static constexpr int A_BYTES = MODE == VD_HALF ? T2_A_BYTES / 2 : T2_A_BYTES;
-    static constexpr int RING_BYTES = PAIR ? (KIND == VD_L ? 6 : KIND == VD_R ? 3 : 5) * T2_STAGE_BYTES : (STORES ? 160 : 224) * 1024;
+    static constexpr int RING_BYTES = PAIR ? (KIND == VD_L ? 6 : KIND == VD_R ? 3 : 5) * T2_STAGE_BYTES
+                                           : (STORES ? 160 : 224) * 1024;
     static constexpr int STAGES = PAIR ? RING_BYTES / T2_STAGE_BYTES : 12;       // single CTAs: at most, as many as fit the tile's width
     static constexpr int SMEM_BYTES = RING_BYTES + 2 * BOXES * 16384 + 1024 /*align*/ + TC_BAR_BYTES;
     static int stages(int width) {
@@ -482,12 +500,16 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 if (lane == 0) vd_arrive<PAIR>(tempty_bar(it & 1));
                 ++it;
                 if constexpr (KIND == VD_X)
-                    if (!Tr::STORES || args.dx32) {                      // (whole 128-byte lines of 32 columns, a row per lane)
-                        float* out = args.dx32 + ((size_t)(t / tiles) * args.N + row) * args.pitch + col0;
-                        if (mine)
+                    if (!Tr::STORES || args.dx32) {
+                        const int row0 = row - lane;
+                        float* out = args.dx32 + ((size_t)(t / tiles) * args.N + row0) * args.pitch + col0;
+                        float* sh = reinterpret_cast<float*>(boxes) + (warp - 2) * (ROW_STAGE_BYTES / 4);    // (pairs: the boxes' room)
 #pragma unroll
-                            for (int g = 0; g < 4; ++g)
-                                if (col0 + 32 * g < min(args.pitch, tile_end)) epi_f32<32>(out + 32 * g, y[g], args.accumulate);
+                        for (int g = 0; g < 4; ++g) {
+                            if (col0 + 32 * g >= min(args.pitch, tile_end)) continue;
+                            if constexpr (PAIR) store_rows_32(sh, y[g], out + 32 * g, args.pitch, min(32, args.N - row0), 32, args.accumulate != 0, lane);
+                            else if (mine) epi_f32<32>(out + (size_t)lane * args.pitch + 32 * g, y[g], args.accumulate);
+                        }
                         continue;
                     }
                 const bool issuer = quarter == 0 && lane == 0;
