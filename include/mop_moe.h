@@ -257,6 +257,7 @@ mop_status mop_moe_route_bwd(mop_ctx* ctx, const float* logits, const float* bia
  *   p[t,e]      = softmax_e(z[t,:])   |   sigmoid(z[t,e]) / sum_e' sigmoid(z[t,e'])         (score_fn)
  *   counts[s,e] = number of picks topk_idx[t,j] = e of the sequence's tokens;   prob[s,e] = 1 / T_s sum_t p[t,e]
  *   loss[s]     = E / (k T_s) sum_e counts[s,e] prob[s,e]                 (1 when every expert gets the same share)
+ * Two calls that may overlap on the GPU (other streams, other graphs) need contexts and workspaces of their own, as everywhere here.
  * A sequence without tokens has zero counts, prob and loss.  A logit of -inf masks an expert; a token whose experts are all masked
  * adds nothing to prob.  Picks outside [0,E) are not counted.
  * logits [T,E] f32 (from mop_moe_route); topk_idx [T,k]; seq_offsets [n_seq+1] i32, non-decreasing within [0,T], or NULL with
@@ -382,7 +383,7 @@ mop_status mop_vocab_loss_bwd(int device, int32_t N, int32_t H, int32_t V, const
  * and the logits at the teacher's places.  A place that is named more than once counts each time.
  * X [N,H] bf16; W_voc [H,V] bf16; teacher_idx [N,K] i32; teacher_logits [N,K] f32; teacher_lse_opt [N] f32 or NULL; temperature > 0;
  * loss [N] f32, student [N,K] f32 (Y at the teacher's places, 0 for ignored entries), lse [N] f32 out.  H and V must be multiples
- * of 8, 1 <= K <= 256.  workspace: mop_vocab_distill_workspace_bytes bytes of device memory, 256-byte aligned, owned by the caller;
+ * of 8, 1 <= K <= 256.  Calls that may overlap on the GPU need workspaces of their own.  workspace: mop_vocab_distill_workspace_bytes bytes of device memory, 256-byte aligned, owned by the caller;
  * mop_vocab_poll reads it as for the calls above. */
 size_t mop_vocab_distill_workspace_bytes(int32_t N, int32_t H, int32_t V, int32_t K);
 mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, int32_t K, const void* X, const void* W_voc,

@@ -365,3 +365,42 @@ def test_a_training_step_of_the_layer_with_the_balance_loss(score, mode):
         assert ((got.double() - was - grad).abs() <= step * (was + grad).abs() + (2.0 ** -9 if step > 1e-6 else 1e-4) * grad.abs().max()).all()
     if mode == PRE:
         assert torch.allclose(dbias.double() - before[1], b.grad, rtol=1e-4, atol=1e-6 * float(before[1].abs().max()))
+
+
+def test_logits_beyond_31_bits():
+    """T E > 2^31: counts and means of everything, gradients of the last rows and dW_r of everything, against fp64 on the device."""
+    T, E, d = (1 << 21) + 4100, 1024, 64
+    ctx = binding.Context(T, d, E, 1, 64, SIGMOID, NONE)
+    g = torch.Generator(device="cuda").manual_seed(40)
+    logits = torch.empty((T, E), device="cuda").normal_(generator=g)
+    idx = torch.randint(0, E, (T, 1), generator=g, device="cuda", dtype=torch.int32)
+    x = torch.randn((T, d), generator=g, device="cuda").to(torch.bfloat16)
+    W_r = torch.randn((d, E), generator=g, device="cuda") * 0.05
+    offs = torch.tensor([0, T - 3000, T], dtype=torch.int32, device="cuda")
+    counts = torch.empty((2, E), dtype=torch.int32, device="cuda")
+    prob, loss = torch.empty((2, E), device="cuda"), torch.empty((2,), device="cuda")
+    ws = torch.empty(max(binding.mop_moe_balance_workspace_bytes(ctx, 2, b) for b in (False, True)), dtype=torch.uint8, device="cuda")
+    binding.mop_moe_balance_loss_fwd(ctx, logits, None, idx, offs, counts, prob, loss, ws)
+    dloss = torch.tensor([3000.0, 1.0], device="cuda")
+    dW, dX = torch.empty((d, E), device="cuda"), torch.empty((T, d), device="cuda", dtype=torch.bfloat16)
+    binding.mop_moe_balance_loss_bwd(ctx, logits, None, offs, counts, dloss, x, W_r, None, dW, None, dX, False, ws)
+    binding.mop_poll(ctx)
+    total, want_dW, terms = torch.zeros(E, device="cuda", dtype=torch.float64), torch.zeros((d, E), device="cuda", dtype=torch.float64), 0.0
+    for s, (a, b) in enumerate(((0, T - 3000), (T - 3000, T))):
+        assert torch.equal(counts[s], torch.bincount(idx[a:b, 0].long(), minlength=E).to(torch.int32))
+        c = dloss[s].double() * E / float(b - a) ** 2 * counts[s].double()
+        total.zero_()
+        for r in range(a, b, 1 << 17):
+            z = torch.sigmoid(logits[r:min(b, r + (1 << 17))].double())
+            p = z / z.sum(1, keepdim=True)
+            total += p.sum(0)
+            dz = p * (1 - z) * (c - (p * c).sum(1, keepdim=True))
+            xs = x[r:min(b, r + (1 << 17))].double()
+            want_dW += xs.T @ dz
+            terms = terms + xs.abs().T @ (dz.abs() + p * (c - c.mean()).abs())
+        # (7100 tokens a block, 444 for a warp of its sixteen, 296 blocks over four slices: 444 + 16 + 74 + 4 half steps at most)
+        assert float((prob[s].double() * (b - a) / total - 1).abs().max()) <= 538 * 2.0 ** -24 + 1.5e-6
+        want = (dz @ W_r.double().T)[-3000:]
+        got = dX[b - want.shape[0]:b].double()
+        assert bool(((got - want).abs() <= 2.0 ** -8 * want.abs() + 2.0 ** -9 * (dz[-3000:].abs() @ W_r.double().abs().T)).all())
+    assert bool(((dW.double() - want_dW).abs() <= 1e-5 * terms).all())

@@ -282,6 +282,41 @@ def test_full_size_sampled_rows_and_invariant():
         assert float((part.sum(1).abs() / part.abs().sum(1)).max()) < 2.0 ** -8
 
 
+@pytest.mark.parametrize("N,H,V", [(5, 7168, 409600), (33000, 64, 131072)], ids=["weights", "logits"])
+def test_weights_and_logits_beyond_31_bits(N, H, V):
+    """H V, or N V, > 2^31, against fp64 on the device in slabs of the vocabulary; entries at the far end."""
+    K, tau = 8, 1.0
+    X, W, ids, t, dloss = inputs(N, H, V, K, seed=N, std=2.0 / H ** 0.5)
+    ids[:, -1] = V - 1 - torch.arange(N, device="cuda", dtype=torch.int32) % 100
+    loss, student, lse, _ = forward(X, W, ids, t, tau)
+    dX, dW, ws = backward(X, W, ids, t, tau, student, lse, dloss)
+    binding.mop_vocab_poll(0, ws)
+    x, step = X.double(), 1 << 13
+    ref = torch.full((N,), -float("inf"), device="cuda", dtype=torch.float64)
+    picked = torch.zeros((N, K), device="cuda", dtype=torch.float64)
+    for v in range(0, V, step):
+        Y = x @ W[:, v:v + step].double()
+        ref = torch.logaddexp(ref, torch.logsumexp(Y, 1))
+        here = (ids >= v) & (ids < v + step)
+        picked = torch.where(here, Y.gather(1, (ids - v).clamp(0, Y.shape[1] - 1).long()), picked)
+    far = SUM_TOL * 12 * H ** 0.5 * float(x.abs().max())          # sum |x| |w|: w has 2 / sqrt(H)
+    assert float((student.double() - picked).abs().max()) <= far
+    assert float((lse.double() - ref).abs().max()) <= far + 4e-6 + 2.0 ** -22 * float(ref.abs().max())
+    q = torch.softmax(t.double(), 1)
+    want_dX, err, norm = torch.zeros_like(x), 0.0, 0.0
+    for v in range(0, V, step):
+        w = W[:, v:v + step].double()
+        dY = (x @ w - ref[:, None]).exp()
+        here = (ids >= v) & (ids < v + step)
+        dY.scatter_add_(1, torch.where(here, ids - v, 0).long(), torch.where(here, -q, 0.0))
+        dY *= dloss.double()[:, None]
+        want_dX += dY @ w.T
+        want = x.T @ dY
+        err, norm = err + float((dW[:, v:v + step].double() - want).square().sum()), norm + float(want.square().sum())
+    assert (err / norm) ** 0.5 <= 4e-3
+    assert float((dX.double() - want_dX).norm() / want_dX.norm()) <= 4e-3
+
+
 def test_refusals():
     N, H, V, K = 64, 64, 128, 5
     X, W, ids, t, dloss = inputs(N, H, V, K, seed=16)
