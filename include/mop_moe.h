@@ -383,7 +383,8 @@ mop_status mop_vocab_loss_bwd(int device, int32_t N, int32_t H, int32_t V, const
  * and the logits at the teacher's places.  A place that is named more than once counts each time.
  * X [N,H] bf16; W_voc [H,V] bf16; teacher_idx [N,K] i32; teacher_logits [N,K] f32; teacher_lse_opt [N] f32 or NULL; temperature > 0;
  * loss [N] f32, student [N,K] f32 (Y at the teacher's places, 0 for ignored entries), lse [N] f32 out.  H and V must be multiples
- * of 8, 1 <= K <= 256.  Calls that may overlap on the GPU need workspaces of their own.  workspace: mop_vocab_distill_workspace_bytes bytes of device memory, 256-byte aligned, owned by the caller;
+ * of 8, V <= 2^30, 1 <= K <= 256.  X and W_voc have to be finite, in the rows of tokens without entries too (their gradient is 0 times
+ * them).  Calls that may overlap on the GPU need workspaces of their own.  workspace: mop_vocab_distill_workspace_bytes bytes of device memory, 256-byte aligned, owned by the caller;
  * mop_vocab_poll reads it as for the calls above. */
 size_t mop_vocab_distill_workspace_bytes(int32_t N, int32_t H, int32_t V, int32_t K);
 mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, int32_t K, const void* X, const void* W_voc,

@@ -836,7 +836,7 @@ __global__ void __launch_bounds__(256) balance_dx_kernel(const float* __restrict
                                                          bf16* __restrict__ dX, int T, int d, int E, int accumulate) {
     pdl_begin();
     __shared__ float sz[64][17], sw[64][17];
-    const int i0 = blockIdx.x * 64, t0 = blockIdx.y * 64, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
+    const int i0 = blockIdx.y * 64, t0 = blockIdx.x * 64, tx = threadIdx.x % 16, ty = threadIdx.x / 16;
     const int begin = bal_off(q, 0), end = bal_off(q, q.S);
     float acc[4][4] = {};
     for (int e0 = 0; e0 < E; e0 += 16) {

@@ -403,7 +403,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 VdScan scan;
                 (void)en; (void)scan;
                 if constexpr (PAIR) en.open(args, row, col0, min(col0 + 128, tile_end), mine && col0 < tile_end);
-                else scan.open(args.lists, quarter * 32, min(32, max(0, args.N - quarter * 32)), col0, min(col0 + 128, tile_end), lane);
+                else scan.open(args.lists, quarter * 32, col0 < tile_end ? min(32, max(0, args.N - quarter * 32)) : 0, col0, min(col0 + 128, tile_end), lane);
                 float y[4][32];
 #pragma unroll
                 for (int g = 0; g < 4; ++g)

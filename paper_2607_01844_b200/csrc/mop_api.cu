@@ -1331,7 +1331,7 @@ mop_status mop_moe_balance_loss_bwd(mop_ctx* c, int32_t n_seq, const float* logi
         if (r == MOP_OK) r = after_launch(c);
     } else if (dX_opt) {
         LAUNCH(c, "balance_dx", st,
-               pdl_launch(balance_dx_kernel, dim3(ceil_div(s.d, 64), ceil_div(s.T, 64)), 256, 0, st, a.dz, W_r, a.q,
+               pdl_launch(balance_dx_kernel, dim3(ceil_div(s.T, 64), ceil_div(s.d, 64)), 256, 0, st, a.dz, W_r, a.q,
                           static_cast<bf16*>(dX_opt), s.T, s.d, s.E, accumulate));
         r = after_launch(c);
     }
@@ -1907,7 +1907,10 @@ mop_status distill_check(int device, int32_t N, int32_t H, int32_t V, int32_t K,
     if (N < 0 || H < 1 || V < 1 || K < 1 || !(temperature > 0.0f) || !(temperature < INFINITY)) return MOP_ERR_INVALID_ARG;
     if (device < 0 || device >= kMaxDevices) return MOP_ERR_INVALID_ARG;
     if (H % 8 || V % 8) return MOP_ERR_ALIGN;
-    if (K > VD_MAX_K || (long long)N * 2 >= (1ll << 31) || (long long)H * V >= (1ll << 40)) return MOP_ERR_SHAPE;
+    if (K > VD_MAX_K || V > (1 << 30) || (long long)N * 2 >= (1ll << 31) || (long long)H * V >= (1ll << 40)) return MOP_ERR_SHAPE;
+    // (tiles and units of work are counted in 32 bits: rows by columns of the logits, and of dX with its ranges)
+    const long long rows = N / 256 + 1;
+    if (rows * (V / 128 + 1) >= (1ll << 31) || rows * (H / 256 + 1) * VD_MAX_SPLITS >= (1ll << 31)) return MOP_ERR_SHAPE;
     return MOP_OK;
 }
 bool distill_sizes_ok(int32_t N, int32_t H, int32_t V, int32_t K) { return distill_check(0, N, H, V, K, 1.0f) == MOP_OK; }

@@ -243,7 +243,8 @@ def test_nothing_is_written_outside_the_outputs_and_the_workspaces():
 
 @pytest.mark.parametrize("N,H,V", [(33000, 72, 16384 + 72),       # three blocks of columns, the last one shorter and of no whole chunk
                                    (33001, 328, 8192 + 8),        # two
-                                   (700, 2048, 4096)],            # one block, dX in one range: stored at once
+                                   (700, 2048, 4096),             # one block, dX in several ranges
+                                   (2304, 2040, 4096)],           # one block, dX in one range: stored at once
                          ids=lambda v: str(v))
 def test_blocks_of_columns_against_fp64_on_the_device(N, H, V):
     K, tau = 50, 1.5
