@@ -92,6 +92,9 @@ __device__ __forceinline__ void bal_scores(const BalShape& s, float (&z)[4 * NV]
 }
 
 // ------------------------------------------------------------------------------------------ forward
+// Bound by latency: T 16384, E 256 takes 12 us for 17.8 MB (a launch, the search for the block's sequence, three or four rounds of one
+// row per warp, 16 warps' sums through shared memory), T 256, E 8 in one block 5.8.  In a training loop the calls themselves, 16 us,
+// take longer than either.
 // Sequences are cut where blocks of `chunk` tokens end.  A block finishes the sequences that lie inside its chunk; of one that goes
 // on beyond it, it leaves the sums: slot 0 where the sequence began before the chunk, slot 1 where it begins in it.
 struct BalFwdArgs {
@@ -214,62 +217,83 @@ __global__ void __launch_bounds__(512) balance_fwd_kernel(const BalFwdArgs a) {
     }
 }
 
-// The sequences that several blocks hold a part of, and those without tokens.  Thread (slice, vector) adds every slices-th block's sums
-// of four experts (of one where the rows are no whole vectors).
-constexpr int BF_THREADS = 1024;
+// The sequences that several blocks hold a part of, and those without tokens: a cluster each, whose CTAs share the experts (the
+// partial sums of a long batch are 600 KB at 256 experts, 5 us for one SM alone: 11.3 us in one CTA, 7.6 in eight).  Thread (slice, vector) adds every
+// slices-th block's sums of four experts (of one where the rows are no whole vectors); the CTAs' shares of the loss meet in the first
+// one's shared memory.
+constexpr int BF_THREADS = 512, BF_CLUSTER = 8;
 __global__ void __launch_bounds__(BF_THREADS) balance_finish_kernel(const BalFwdArgs a) {
     pdl_begin();
-    __shared__ float sh[32];
+    __shared__ float sh[32], share[BF_CLUSTER];
     __shared__ __align__(16) float sp[4 * BF_THREADS];
     __shared__ __align__(16) int32_t sc[4 * BF_THREADS];
-    const int E = a.s.E, per = a.s.vec4 ? 4 : 1, vecs = E / per, slices = BF_THREADS / vecs;      // (E is at most 1024)
-    const int vec = threadIdx.x % vecs, slice = threadIdx.x / vecs, tid = threadIdx.x;
-    for (int seq = blockIdx.x; seq < a.q.S; seq += gridDim.x) {
+    uint32_t ctas;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(ctas));
+    const uint32_t rank = cluster_ctarank();
+    const int E = a.s.E, per = a.s.vec4 ? 4 : 1, all = E / per, mine = (all + (int)ctas - 1) / (int)ctas;
+    const int v0 = min(all, (int)rank * mine), vecs = max(1, min(all, v0 + mine) - v0);      // (a CTA without any repeats one, unused)
+    const int e0 = v0 * per, ne = (min(all, v0 + mine) - v0) * per;
+    const int slices = BF_THREADS / vecs, vec = threadIdx.x % vecs, slice = threadIdx.x / vecs, tid = threadIdx.x, row = vecs * per;
+    for (int seq = blockIdx.x / ctas; seq < a.q.S; seq += gridDim.x / ctas) {
         const int first = bal_off(a.q, seq), last = bal_off(a.q, seq + 1);
         const int b0 = first / a.chunk, b1 = (last - 1) / a.chunk;
-        if (last > first && b0 == b1) continue;                           // done by its block
-        float4 p = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        int4 c = make_int4(0, 0, 0, 0);
-        if (last > first && slice < slices) {
-            if (per == 4) {
-#pragma unroll 6
-                for (int b = b0 + slice; b <= b1; b += slices) {
-                    const size_t slot = ((size_t)b * 2 + (b == b0 ? 1 : 0)) * E + 4 * vec;
-                    const float4 x = *reinterpret_cast<const float4*>(a.part_p + slot);
-                    const int4 y = *reinterpret_cast<const int4*>(a.part_c + slot);
-                    p.x += x.x; p.y += x.y; p.z += x.z; p.w += x.w;
-                    c.x += y.x; c.y += y.y; c.z += y.z; c.w += y.w;
-                }
-            } else {
-#pragma unroll 8
-                for (int b = b0 + slice; b <= b1; b += slices) {
-                    const size_t slot = ((size_t)b * 2 + (b == b0 ? 1 : 0)) * E + vec;
-                    p.x += a.part_p[slot];
-                    c.x += a.part_c[slot];
-                }
-            }
-        }
-        if (slice < slices) {
-            if (per == 4) {
-                *reinterpret_cast<float4*>(sp + 4 * tid) = p;
-                *reinterpret_cast<int4*>(sc + 4 * tid) = c;
-            } else { sp[tid] = p.x; sc[tid] = c.x; }
-        }
-        __syncthreads();
+        if (last > first && b0 == b1) continue;                           // done by its block (for every CTA of the cluster alike)
         float dot = 0.0f;
         const float n = (float)max(1, last - first);
-        if (tid < E) {                                                    // slice i holds its sums E further on
-            float q = 0.0f;
-            int32_t d = 0;
-            for (int i = 0; i < slices; ++i) { q += sp[i * E + tid]; d += sc[i * E + tid]; }
-            q /= n;
-            a.prob[(size_t)seq * E + tid] = q;
-            a.counts[(size_t)seq * E + tid] = d;
-            dot = (float)d * q;
+        {
+            float4 p = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            int4 c = make_int4(0, 0, 0, 0);
+            if (last > first && slice < slices && ne > 0) {
+                if (per == 4) {
+#pragma unroll 6
+                    for (int b = b0 + slice; b <= b1; b += slices) {
+                        const size_t slot = ((size_t)b * 2 + (b == b0 ? 1 : 0)) * E + e0 + 4 * vec;
+                        const float4 x = *reinterpret_cast<const float4*>(a.part_p + slot);
+                        const int4 y = *reinterpret_cast<const int4*>(a.part_c + slot);
+                        p.x += x.x; p.y += x.y; p.z += x.z; p.w += x.w;
+                        c.x += y.x; c.y += y.y; c.z += y.z; c.w += y.w;
+                    }
+                } else {
+#pragma unroll 8
+                    for (int b = b0 + slice; b <= b1; b += slices) {
+                        const size_t slot = ((size_t)b * 2 + (b == b0 ? 1 : 0)) * E + e0 + vec;
+                        p.x += a.part_p[slot];
+                        c.x += a.part_c[slot];
+                    }
+                }
+            }
+            if (slice < slices) {
+                if (per == 4) {
+                    *reinterpret_cast<float4*>(sp + 4 * tid) = p;
+                    *reinterpret_cast<int4*>(sc + 4 * tid) = c;
+                } else { sp[tid] = p.x; sc[tid] = c.x; }
+            }
+            __syncthreads();
+            for (int e = tid; e < ne; e += BF_THREADS) {                  // slice i holds its sums `row` further on
+                float q = 0.0f;
+                int32_t d = 0;
+                for (int i = 0; i < slices; ++i) { q += sp[i * row + e]; d += sc[i * row + e]; }
+                q /= n;
+                a.prob[(size_t)seq * E + e0 + e] = q;
+                a.counts[(size_t)seq * E + e0 + e] = d;
+                dot = fmaf((float)d, q, dot);
+            }
         }
         dot = bal_block_sum(dot, sh);
-        if (tid == 0) a.loss[seq] = dot * ((float)E / ((float)a.s.k * n));
-        __syncthreads();
+        if (tid == 0) {
+            uint32_t to;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to) : "r"((uint32_t)__cvta_generic_to_shared(share + rank)));
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(dot) : "memory");
+        }
+        __syncwarp();
+        cluster_sync_all();
+        if (tid == 0 && rank == 0) {
+            float total = 0.0f;
+            for (uint32_t i = 0; i < ctas; ++i) total += share[i];
+            a.loss[seq] = total * ((float)E / ((float)a.s.k * n));
+        }
+        __syncwarp();
+        cluster_sync_all();                       // (also: nobody leaves while another may still write to it)
     }
 }
 
@@ -343,6 +367,8 @@ __device__ __forceinline__ void bal_copy_edge(const BalBwdArgs& a, int edge, int
     }
 }
 
+// T 16384, d 7168, E 256: 24 us for 17 MB in and 41 MB out, beside it 7.3 MB of W_r; rounds of about a microsecond, three blocks of eight
+// warps on an SM.
 // dz, zero for tokens outside the sequences.  Counts are taken relative to their mean (k T_s / E, rounded): c_e - sum p c does not
 // change by a shift, and under a nearly balanced load, which this loss aims at, the difference keeps its digits.
 // The blocks behind the first dz_blocks prepare W_r and the edges of x.
@@ -486,8 +512,10 @@ __global__ void __launch_bounds__(256, NV <= 2 ? 3 : NV == 4 ? 2 : 1) balance_dz
 // is added up in segments of BW_SEG blocks, because the tensor core truncates where it adds.
 //
 // Few tiles, long sums: the token blocks of all tiles are laid in a row and cut into equal ranges, one for each pair.  A tile that one
-// range covers goes to dW_r at once; of one that is cut, each range leaves its sums, and balance_dw_sum_kernel adds them in order.
+// range covers goes to dW_r at once; of one that is cut, each range leaves its sums, and balance_sum_kernel adds them in order.
 // T 16384, d 7168, E 256: 28 tiles of 256 blocks are 97 blocks for each pair (five equal ranges per tile made 104, and 140 sums).
+// 122 us there, 180 GFLOP of issued products at 1.48 PFLOP/s: the tensor cores are busy for 84 % of a CTA's time, at 1.6 GHz.
+// Two pieces would take a third less, at 2.4e-6 of dW_r's norm instead of the fp32 accuracy that the router's own gradient has.
 constexpr int BW_SA = 3, BW_SB = 9, BW_SLOT = 16384, BW_SEG = 3, BW_EPI_WARPS = 8;
 constexpr int BW_THREADS = 64 + 32 * BW_EPI_WARPS;
 constexpr int BW_SMEM_BYTES = (BW_SA + BW_SB) * BW_SLOT + BW_EPI_WARPS * ROW_STAGE_BYTES + 1024 /*align*/ + TC_BAR_BYTES;

@@ -1226,7 +1226,8 @@ mop_status mop_moe_balance_loss_fwd(mop_ctx* c, int32_t n_seq, const float* logi
 #undef GO
     mop_status r = after_launch(c);
     if (r != MOP_OK || blocks == 1) return r;
-    LAUNCH(c, "balance_finish", st, pdl_launch(balance_finish_kernel, min(n_seq, 1184), BF_THREADS, 0, st, a));
+    const int ctas = n_seq < 64 || s.E > 512 ? BF_CLUSTER : 1;        // (many sequences keep the SMs busy by themselves)
+    LAUNCH(c, "balance_finish", st, pdl_launch_clusters(balance_finish_kernel, ctas, min(n_seq, 1184 / ctas) * ctas, BF_THREADS, 0, st, a));
     return after_launch(c);
 }
 

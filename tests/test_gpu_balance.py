@@ -136,6 +136,9 @@ LAYERS = [
     (90, 64, 1000, 32, SOFTMAX, NONE, [0, 40, 90]),
     (64, 64, 1024, 32, SIGMOID, PRE, None),
     (50, 64, 7, 7, SOFTMAX, NONE, [20, 20, 20]),                          # no token belongs to a sequence
+    (2000, 64, 3, 2, SIGMOID, NONE, [0, 1000, 1990]),                     # fewer vectors than CTAs that finish a sequence
+    (1500, 64, 1001, 4, SOFTMAX, NONE, [0, 0, 700, 1500]),                # an odd number of experts for each of them
+    (1300, 64, 600, 4, SOFTMAX, PRE, [13 * i for i in range(100)]),       # many sequences and many experts
 ]
 
 
