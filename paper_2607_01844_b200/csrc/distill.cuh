@@ -6,13 +6,21 @@
 //
 // vd_gemm_kernel runs the products, with eight epilogue warps behind a TMA producer and an MMA issuer:
 //   VD_L  Y = X W_voc: per row and up to 128 columns the maximum and the sum of exponentials, and the logits of the teacher's entries
-//   VD_P  dY, one block of vocabulary columns, bf16 (the only piece of the N x V matrix that ever exists)
+//   VD_P  dY, one block of vocabulary columns, bf16 (the only piece of the N x V matrix that ever exists); with up to 128 rows two
+//         pieces, dY = hi + lo
 //   VD_X  dX = dY W_voc^T: the block's columns (its K) in `splits` ranges, fp32 sums over the blocks
 //   VD_W  dW_voc[:, block] = X^T dY, bf16, beside VD_X
 //   VD_R  the router's dX (+)= dz W_r^T (balance.cuh) from fp16 operands that are scaled by powers of two, bf16
 // With many rows on CTA pairs (256 x 256 tiles, tcgen05.mma.cta_group::2, stages of 64 of K, as tc_gemm2_kernel).  With up to 128 rows
 // a pair would multiply as much again in vain, and half of its stages would hold X: reading W is all there is then, and the product
 // runs on single CTAs, tiles of 128 rows and up to 256 columns, whose rings hold as many bytes of W in flight as shared memory takes.
+//
+// One bf16 dY has an error of up to 2^-8 in each of its elements.  In the gradients these average out over the tokens, to about what the
+// rounding of the gradients themselves costs, but with few tokens they are the error of one or two elements that outweigh the rest
+// (temperature 1, H 512, V 16384, K 5 to 126, error of dX over that of rounding it once: 1.4 in the middle, up to 1.9 with 2 tokens, 1.6
+// with 16, 1.5 with 64 to 128, 1.49 with 192; 1.00 with two pieces).  There the products wait for W, and a second piece with what the first
+// leaves out costs less than its operations (backward in us, one piece and two: N 10, H 1936, V 28800 86, 90; N 16, H 4096, V 64000 300,
+// 305; N 64, H 2048, V 32000 100, 108; N 100, H 2048, V 50304 150, 170; N 128, H 7168, V 131072 1028, 1249).
 //
 // What bounds them, measured: many rows the tensor cores (VD_L N 2048, H 2048, V 32000 177 us, 1.52 PFLOP/s, where cuBLAS takes 180 for
 // the same product with its bf16 store; N 8192, H 7168, V 131072 11.8 to 13.4 ms under the power cap, cuBLAS 11.1); few rows DRAM (VD_L
@@ -58,7 +66,7 @@ enum : int { VD_PAIR = 0, VD_ONE = 1, VD_HALF = 2 };
 template <int KIND, int MODE>
 struct VdTraits {
     static constexpr bool PAIR = MODE == VD_PAIR;
-    static constexpr bool STORES = KIND != VD_L && (PAIR || KIND != VD_X);       // (a single CTA's VD_X has several ranges)
+    static constexpr bool STORES = KIND != VD_L && (PAIR || KIND != VD_X);       // (a single CTA's VD_X has two pieces to add up)
     static constexpr int SETS = KIND == VD_R ? 2 : 1;         // pairs of boxes
     static constexpr int BOXES = STORES ? 2 * SETS : 0;
     static constexpr int A_BYTES = MODE == VD_HALF ? T2_A_BYTES / 2 : T2_A_BYTES;
@@ -93,6 +101,7 @@ struct VdArgs {
     int k_base;                   // VD_X: the same, added to W's K coordinate
     int cols;                     // columns of the whole output that exist
     int a_split, b_split;         // that operand's columns are no multiple of 64: one copy per 64-wide chunk, whose edge is zero-filled
+    int piece_rows;               // dY has two pieces (maps of [2][N][columns]), of which a tile holds as many rows each: 64, 128, or 0: one
     int splits;                   // VD_X: ranges of K, as separate units of work (1 elsewhere)
     float c;                      // log2(e) / tau
     const int2* entry;            // [N, K] the row's entries by column (ascending): {column, place in the caller's list (VD_L) or dY (VD_P)}
@@ -109,7 +118,7 @@ struct VdArgs {
     bf16* add_to;                 // VD_R: dX [N, cols] that the product is added to, or null
     const int32_t* seq_off;       // VD_R: offsets of the sequences or null: rows outside [seq_off[0], seq_off[n_seq]) keep what they hold
     int n_seq;
-    float* dx32;                  // VD_X: [splits, N, pitch] fp32 sums, or null (pairs only): one range and one block, dX is stored at once
+    float* dx32;                  // VD_X: [splits (x 2 with two pieces), N, pitch] fp32 sums, or null (pairs only): one range and one block, dX is stored at once
     int pitch, accumulate;        // VD_X: add to them
     int32_t* status;
     bool gemm_follows;
@@ -155,6 +164,22 @@ struct VdEntries {
         return r;
     }
 };
+
+// Eight values as bf16; what the rounding leaves out stays behind (nothing, where they are not finite).
+__device__ __forceinline__ uint4 pack_and_keep_rest(float* v) {
+    const uint4 r = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float rest = v[i] - (i % 2 ? bf16_hi(w[i / 2]) : bf16_lo(w[i / 2]));
+        v[i] = fabsf(rest) < INFINITY ? rest : 0.0f;
+    }
+    return r;
+}
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                 :: "l"(reinterpret_cast<uint64_t>(map)), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+}
 
 // The primitives on a pair (completing on, or signalling, both CTAs' or the leader's barriers) and on a single CTA.
 template <bool PAIR>
@@ -242,7 +267,7 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                const VdArgs args) {
     using Tr = VdTraits<KIND, MODE>;
     constexpr bool PAIR = Tr::PAIR;
-    static_assert(PAIR || KIND == VD_L || KIND == VD_P || KIND == VD_X, "the kinds whose rows are few tokens");
+    static_assert(PAIR || KIND == VD_L || KIND == VD_P || (KIND == VD_X && MODE == VD_ONE), "the kinds whose rows are few tokens");
     constexpr int S = Tr::STAGES;
     constexpr int TM = PAIR ? 256 : 128;
     constexpr bool A_MN = KIND == VD_W;                       // the tokens are K: X^T lies with M contiguous
@@ -328,13 +353,17 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 const int k0 = kb * TC_BK;
                 if (el) {
                     if (leader) mbar_expect_tx(full_bar(stage), (PAIR ? 2 : 1) * copy_bytes);
-                    if constexpr (!A_MN) vd_load_2d<PAIR>(sA, &tmA, fb, k0, m0);
-                    else if (!args.a_split) vd_load_3d<PAIR>(sA, &tmA, fb, 0, k0, m0 >> 6);
+                    // two pieces: the same tokens of X against both; both pieces' rows as the rows of dX's tile
+                    const int ka = KIND == VD_W && args.piece_rows ? k0 % args.piece_rows : k0;
+                    if (KIND == VD_X && args.piece_rows) vd_load_3d<PAIR>(sA, &tmA, fb, k0, 0, (int)rank);
+                    else if constexpr (!A_MN) vd_load_2d<PAIR>(sA, &tmA, fb, k0, m0);
+                    else if (!args.a_split) vd_load_3d<PAIR>(sA, &tmA, fb, 0, ka, m0 >> 6);
                     else {
-                        vd_load_2d<PAIR>(sA, &tmA, fb, m0, k0);
-                        vd_load_2d<PAIR>(sA + TC_CHUNK_BYTES, &tmA, fb, m0 + 64, k0);
+                        vd_load_2d<PAIR>(sA, &tmA, fb, m0, ka);
+                        vd_load_2d<PAIR>(sA + TC_CHUNK_BYTES, &tmA, fb, m0 + 64, ka);
                     }
-                    if constexpr (!B_MN) vd_load_2d<PAIR>(sB, &tmB, fb, k0 + (KIND == VD_X ? args.k_base : 0), n0);
+                    if (KIND == VD_W && args.piece_rows) tma2_load_4d(sB, &tmB, fb, 0, ka, n0 >> 6, k0 / args.piece_rows);
+                    else if constexpr (!B_MN) vd_load_2d<PAIR>(sB, &tmB, fb, k0 + (KIND == VD_X ? args.k_base : 0), n0);
                     else if (!args.b_split) vd_load_3d<PAIR>(sB, &tmB, fb, 0, k0, n0 >> 6);
                     else
                         for (int q = 0; q < my_cols; q += 64) vd_load_2d<PAIR>(sB + q * (TC_CHUNK_BYTES / 64), &tmB, fb, n0 + q, k0);
@@ -508,14 +537,14 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 ++it;
                 if constexpr (KIND == VD_X)
                     if (!Tr::STORES || args.dx32) {
-                        const int row0 = row - lane;
-                        float* out = args.dx32 + ((size_t)(t / tiles) * args.N + row0) * args.pitch + col0;
+                        const int piece = args.piece_rows ? (row - lane) / args.piece_rows : 0, row0 = row - lane - piece * args.piece_rows;
+                        float* out = args.dx32 + ((size_t)(t / tiles * (args.piece_rows ? 2 : 1) + piece) * args.N + row0) * args.pitch + col0;
                         float* sh = reinterpret_cast<float*>(boxes) + (warp - 2) * (ROW_STAGE_BYTES / 4);    // (pairs: the boxes' room)
 #pragma unroll
                         for (int g = 0; g < 4; ++g) {
                             if (col0 + 32 * g >= min(args.pitch, tile_end)) continue;
                             if constexpr (PAIR) store_rows_32(sh, y[g], out + 32 * g, args.pitch, min(32, args.N - row0), 32, args.accumulate != 0, lane);
-                            else if (mine) epi_f32<32>(out + (size_t)lane * args.pitch + 32 * g, y[g], args.accumulate);
+                            else if (row0 + lane < args.N) epi_f32<32>(out + (size_t)lane * args.pitch + 32 * g, y[g], args.accumulate);
                         }
                         continue;
                     }
@@ -550,6 +579,42 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                             }
                         }
                     }
+                }
+                if constexpr (KIND == VD_P && !PAIR) {    // the teacher's entries, and two pieces: 64 rows of each in a box, or 128 in turn
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+                        while (en.e[0].x < col0 + 32 * (g + 1)) {
+                            const int2 e = en.take();
+#pragma unroll
+                            for (int q = 0; q < 32; ++q) y[g][q] = e.x - col0 - 32 * g == q ? __int_as_float(e.y) : y[g][q];
+                        }
+#pragma unroll
+                    for (int piece = 0; piece < (MODE == VD_ONE ? 2 : 1); ++piece) {
+                        if (issuer) tma_store_wait_read<0>();
+                        asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+                        if (MODE == VD_ONE || quarter < 2) {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                uint8_t* rowp = box + h * VD_BOX_BYTES + (quarter * 32 + lane) * 128;
+#pragma unroll
+                                for (int j = 0; j < 8; ++j) {
+                                    float* v = &y[2 * h + j / 4][(j % 4) * 8];
+                                    uint8_t* at = rowp + ((j ^ (lane & 7)) << 4);
+                                    *reinterpret_cast<uint4*>(at) = pack_and_keep_rest(v);
+                                    if (MODE == VD_HALF) *reinterpret_cast<uint4*>(at + VD_BOX_BYTES / 2) = pack_and_keep_rest(v);
+                                }
+                            }
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
+                        if (issuer) {
+                            const int x = width * nt + 128 * half, end = min(args.cols, width * (nt + 1));
+                            if (x < end) tma_store_3d(&tmO, smem_u32(box), x, 0, piece);
+                            if (x + 64 < end) tma_store_3d(&tmO, smem_u32(box + VD_BOX_BYTES), x + 64, 0, piece);
+                            tma_store_commit();
+                        }
+                    }
+                    continue;
                 }
                 if (issuer) tma_store_wait_read<Tr::SETS - 1>();          // this pair's last copies have been read
                 asm volatile("bar.sync %0, 128;" ::"r"(1 + half) : "memory");
@@ -855,7 +920,8 @@ inline mop_status vd_init() {
     mop_status r;
     if ((r = vd_set_smem_rows<VD_L>()) != MOP_OK) return r;
     if ((r = vd_set_smem_rows<VD_P>()) != MOP_OK) return r;
-    if ((r = vd_set_smem_rows<VD_X>()) != MOP_OK) return r;
+    if ((r = vd_set_smem<VD_X, VD_PAIR>()) != MOP_OK) return r;
+    if ((r = vd_set_smem<VD_X, VD_ONE>()) != MOP_OK) return r;
     return vd_set_smem<VD_W, VD_PAIR>();
 }
 template <int KIND, int MODE>
@@ -867,6 +933,9 @@ inline mop_status vd_launch(const TcPlan* p, const CUtensorMap& a, const CUtenso
 }
 // The mode by the number of rows.
 inline int vd_mode(int N) { return N <= 64 ? VD_HALF : N <= 128 ? VD_ONE : VD_PAIR; }
+// Rows of a piece of dY in a tile, where it has two; dX's rows are both pieces' then.
+inline int vd_piece_rows(int N) { return vd_mode(N) == VD_HALF ? 64 : vd_mode(N) == VD_ONE ? 128 : 0; }
+inline int vd_mode_x(int N) { return vd_mode(N) == VD_HALF ? VD_ONE : VD_PAIR; }
 inline int vd_row_box(int mode) { return mode == VD_HALF ? 64 : 128; }      // rows of X (or dY) that a CTA copies
 template <int KIND>
 inline mop_status vd_launch_rows(int mode, const TcPlan* p, const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& o, const VdArgs& args,
@@ -891,6 +960,27 @@ inline int vd_width(int mode, int N, int cols) {
     }
     return pick;
 }
+// [2][rows][pitch] of bf16, the first `cols` columns: 64 of them, `box_rows` rows and `box_pieces` pieces at a time.
+inline bool vd_map_pieces(const TcPlan* p, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch, uint32_t box_rows,
+                          uint32_t box_pieces) {
+    const cuuint64_t dims[3] = {cols, rows, 2};
+    const cuuint64_t strides[2] = {pitch * 2, rows * pitch * 2};
+    const cuuint32_t box[3] = {64, box_rows, box_pieces};
+    const cuuint32_t es[3] = {1, 1, 1};
+    return reinterpret_cast<tc_encode_fn>(p->encode)(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, es,
+                                                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// The same in chunks of 64 columns, two chunks and 64 rows of a piece at a time (an operand whose K are the rows).
+inline bool vd_map_pieces_mn(const TcPlan* p, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch) {
+    const cuuint64_t dims[4] = {64, rows, cols / 64, 2};
+    const cuuint64_t strides[3] = {pitch * 2, 128, rows * pitch * 2};
+    const cuuint32_t box[4] = {64, 64, 2, 1};
+    const cuuint32_t es[4] = {1, 1, 1, 1};
+    return reinterpret_cast<tc_encode_fn>(p->encode)(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, es,
+                                                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 // 2-D map over `cols` columns of a bf16 matrix whose rows are `pitch` elements apart, for stores; box = {64 columns, 128 rows}.
 inline bool vd_map_out(const TcPlan* p, CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t pitch) {
     return tc_map_2d_pitch(p, m, base, rows, cols, pitch, 128);
@@ -910,14 +1000,14 @@ inline int vd_block(int N, int V) {
 // each range its sums' way to L2 and back.
 constexpr int VD_MAX_SPLITS = 64;
 inline int vd_splits(int N, int H, int width) {
-    const bool pair = vd_mode(N) == VD_PAIR;
+    const bool pair = vd_mode_x(N) == VD_PAIR, pieces = vd_piece_rows(N) > 0;
     const int workers = pair ? VD_SMS / 2 : VD_SMS;
     const int tiles = (pair ? (N + 255) / 256 : 1) * ((H + 255) / 256), kb = (width + 63) / 64;
-    const double t_sum = 8e-6 * N * H / 5.0;
+    const double t_sum = 8e-6 * N * H / 5.0 * (pieces ? 2 : 1);
     int pick = 1;                             // (what is left of a single K block)
     double best = 1e30;
     for (int s = 1; s <= VD_MAX_SPLITS && s <= kb; ++s) {
-        if (s == 1 && !pair) continue;                    // (their sums go through memory anyway)
+        if (s == 1 && pieces) continue;                   // (their sums go through memory anyway)
         const double t = ((tiles * (long long)s + workers - 1) / workers) * (((kb + s - 1) / s) * 0.3 + 2.0) + (s > 1 ? t_sum * s : 0.0);
         if (t < 0.97 * best) { best = t; pick = s; }
     }

@@ -1873,7 +1873,7 @@ mop_status mop_vocab_loss_bwd(int device, int32_t N, int32_t H, int32_t V, const
 // Distillation from a teacher's top logits through the same projection
 // ---------------------------------------------------------------------------------------------
 namespace {
-struct DistillLayout { size_t status, entry, first, coef, lse2, part, dy, dx32, total; int mode, width, parts, units, vc, blocks, splits, pitch; bool sums; };
+struct DistillLayout { size_t status, entry, first, coef, lse2, part, dy, dx32, total; int mode, width, parts, units, vc, blocks, splits, pitch, piece_rows, pieces; bool sums; };
 DistillLayout distill_layout(int N, int H, int V, int K, bool backward) {
     DistillLayout L{};
     size_t o = 0;
@@ -1897,9 +1897,11 @@ DistillLayout distill_layout(int N, int H, int V, int K, bool backward) {
         L.pitch = ceil_div(H, 32) * 32;   // dX is added up in whole runs of 32 columns
         L.coef = take((size_t)N * 4);
         L.lse2 = take((size_t)N * 4);
-        L.dy = take((size_t)N * L.vc * 2);
-        L.sums = L.blocks > 1 || L.splits > 1 || L.mode != VD_PAIR;
-        if (L.sums) L.dx32 = take((size_t)L.splits * N * L.pitch * 4);
+        L.piece_rows = vd_piece_rows(N);
+        L.pieces = L.piece_rows ? 2 : 1;
+        L.dy = take((size_t)L.pieces * N * L.vc * 2);
+        L.sums = L.blocks > 1 || L.splits > 1 || L.pieces > 1;
+        if (L.sums) L.dx32 = take((size_t)L.splits * L.pieces * N * L.pitch * 4);
     }
     L.total = o;
     return L;
@@ -2002,10 +2004,10 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
     bf16* dY = reinterpret_cast<bf16*>(w + L.dy);
     float* dx32 = L.sums ? reinterpret_cast<float*>(w + L.dx32) : nullptr;
     CUtensorMap mX, mXT, mWn, mWk, mdX;
-    const int box = vd_row_box(L.mode);
-    if (!tc_map_2d(p, &mX, X, N, H, box) || !distill_map_mn(p, &mXT, X, N, H, 128) ||
+    const int mode_x = vd_mode_x(N);
+    if (!tc_map_2d(p, &mX, X, N, H, vd_row_box(L.mode)) || !distill_map_mn(p, &mXT, X, N, H, 128) ||
         !distill_map_mn(p, &mWn, W_voc, H, V, L.mode == VD_PAIR ? L.width / 2 : L.width) ||
-        !tc_map_2d(p, &mWk, W_voc, H, V, L.mode == VD_PAIR ? 128 : 256) || !vd_map_out(p, &mdX, dX, N, H, H))
+        !tc_map_2d(p, &mWk, W_voc, H, V, mode_x == VD_PAIR ? 128 : 256) || !vd_map_out(p, &mdX, dX, N, H, H))
         return MOP_ERR_CUDA;
     DistillPrep a{};
     a.l = {teacher_idx, teacher_logits, teacher_lse_opt, N, V, K, temperature};
@@ -2020,13 +2022,17 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
     for (int c0 = 0; c0 < V; c0 += L.vc) {
         const int cw = V - c0 < L.vc ? V - c0 : L.vc, cw64 = ceil_div(cw, 64) * 64;
         CUtensorMap mdYk, mdYn, mdYo, mdW;
-        if (!tc_map_2d_pitch(p, &mdYk, dY, N, cw, L.vc, box) || !tc_map_chunked_2d_pitch(p, &mdYn, dY, N, cw64, L.vc, 2) ||
-            !vd_map_out(p, &mdYo, dY, N, L.vc, L.vc) || !vd_map_out(p, &mdW, static_cast<bf16*>(dW_voc) + c0, H, cw, V))
+        const bool maps = L.pieces > 1 ? vd_map_pieces(p, &mdYk, dY, N, cw, L.vc, L.piece_rows, 128 / L.piece_rows) &&
+                                             vd_map_pieces_mn(p, &mdYn, dY, N, cw64, L.vc) &&
+                                             vd_map_pieces(p, &mdYo, dY, N, L.vc, L.vc, L.piece_rows, 128 / L.piece_rows)
+                                       : tc_map_2d_pitch(p, &mdYk, dY, N, cw, L.vc, 128) && tc_map_chunked_2d_pitch(p, &mdYn, dY, N, cw64, L.vc, 2) &&
+                                             vd_map_out(p, &mdYo, dY, N, L.vc, L.vc);
+        if (!maps || !vd_map_out(p, &mdW, static_cast<bf16*>(dW_voc) + c0, H, cw, V))
             return MOP_ERR_CUDA;
         const bool last = c0 + L.vc >= V;
         VdArgs base{};
         base.N = N; base.H = H; base.V = V; base.K = K; base.n_group = VOCAB_N_GROUP; base.splits = 1; base.status = status;
-        base.width = 256;
+        base.width = 256; base.piece_rows = L.piece_rows;
         base.gemm_follows = true;
         const PdlNote note = {status + VOCAB_NOTE, c0 / L.vc + 1};
         {   // dY block, logits formed again on the tensor cores
@@ -2043,11 +2049,13 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
             g.splits = min(L.splits, g.kblocks);          // (the first block is the widest and writes the sums of every range)
             g.cols = H; g.dx32 = dx32; g.pitch = L.pitch; g.accumulate = c0 > 0 ? 1 : 0;
             g.note = note;
-            if ((r = vd_launch_rows<VD_X>(L.mode, p, mdYk, mWk, mdX, g, st)) != MOP_OK) return r;
+            r = mode_x == VD_PAIR ? vd_launch<VD_X, VD_PAIR>(p, mdYk, mWk, mdX, g, st) : vd_launch<VD_X, VD_ONE>(p, mdYk, mWk, mdX, g, st);
+            if (r != MOP_OK) return r;
         }
         {   // dW[:, block] = X^T dY (K = the N tokens), written once; its CTAs take over from those of dX (as in mop_vocab_loss_bwd)
             VdArgs g = base;
-            g.tiles_m = ceil_div(H, 256); g.tiles_n = ceil_div(cw, 256); g.kblocks = ceil_div(N, TC_BK);
+            g.tiles_m = ceil_div(H, 256); g.tiles_n = ceil_div(cw, 256);
+            g.kblocks = L.pieces > 1 ? 2 * L.piece_rows / TC_BK : ceil_div(N, TC_BK);
             g.cols = cw; g.a_split = H % 64 != 0; g.note = note;
             g.gemm_follows = !last;                       // the small blocks that follow the last one must not pile up
             if ((r = vd_launch<VD_W, VD_PAIR>(p, mXT, mdYn, mdW, g, st)) != MOP_OK) return r;
@@ -2056,7 +2064,7 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
     if (!dx32) return MOP_OK;
     const size_t blocks_dx = ((size_t)N * (H / 4) + 63) / 64, cap = (size_t)p->sm_count * 16;
     pdl_launch(distill_dx_kernel, (unsigned)(blocks_dx < cap ? blocks_dx : cap), 256, 0, st, dx32, static_cast<bf16*>(dX), N,
-               H, L.pitch, L.splits);
+               H, L.pitch, L.splits * L.pieces);
     return cudaGetLastError() == cudaSuccess ? MOP_OK : MOP_ERR_CUDA;
 }
 

@@ -350,3 +350,32 @@ def test_no_tokens():
     loss, student, lse, _ = forward(X, W, ids, t, 1.0)
     dX, dW, _ = backward(X, W, ids, t, 1.0, student, lse, dloss)
     assert float(dW.abs().max()) == 0.0
+
+
+@pytest.mark.parametrize("N,H,V,K,tau", [(1, 64, 1000, 5, 1.0), (2, 200, 2888, 126, 1.0), (10, 1936, 4104, 126, 1.0), (33, 72, 8200, 64, 0.5), (64, 512, 8192, 31, 1.0),
+                                         (65, 136, 8200, 126, 1.0), (100, 1000, 5000, 64, 4.0), (128, 256, 16384, 9, 1.0),
+                                         (64, 8, (1 << 22) + 520, 4, 1.0), (128, 8, (1 << 21) + 520, 4, 1.0)])     # two blocks of columns
+def test_few_tokens_keep_the_logit_gradients_to_sixteen_bits(N, H, V, K, tau):
+    """Up to 128 tokens dY has two bf16 pieces: 2^-16 of each term is left out.  Sums: the tensor core drops up to 2^-23 of a partial sum in
+    each step of 16, at most 512 steps in a range here (2^-14 of the terms); gradients are rounded once (2^-8).  dY itself is off by what
+    its exponent is: the logits, twice (the sum behind lse, and formed again), 4e-6 + 2^-20 |lse| for lse and its scaling, 6e-6 for the
+    exponential and the products around it, of p and of q."""
+    X, W, ids, t, dloss = inputs(N, H, V, K, seed=N + K, std=2.0 / H ** 0.5)
+    loss, student, lse, _ = forward(X, W, ids, t, tau)
+    dX, dW, ws = backward(X, W, ids, t, tau, student, lse, dloss)
+    binding.mop_vocab_poll(0, ws)
+    x, w = X.double(), W.double()
+    Y = x @ w
+    ref = torch.logsumexp(Y / tau, 1)
+    far = SUM_TOL * float((x.abs() @ w.abs()).max())
+    valid = (ids >= 0) & (ids < V)
+    at = torch.where(valid, ids, 0).long()
+    s = torch.where(valid, t.double() / tau, -float("inf"))
+    q = torch.where(valid, torch.softmax(s, 1), 0.0).nan_to_num(0.0)
+    off = 2 * far / tau + 1e-5 + 2.0 ** -20 * ref.abs()[:, None]
+    p = torch.exp(Y / tau - ref[:, None]) * q.sum(1, keepdim=True)
+    size = p.scatter_add(1, at, q) * (dloss.double().abs()[:, None] / tau) * off
+    dY = p.scatter_add(1, at, -q) * (dloss.double()[:, None] / tau)
+    del Y, p
+    for got, want, terms, base in ((dX, dY @ w.T, dY.abs() @ w.abs().T, size @ w.abs().T), (dW, x.T @ dY, x.abs().T @ dY.abs(), x.abs().T @ size)):
+        assert bool(((got.double() - want).abs() <= 2.0 ** -8 * want.abs() + (2.0 ** -16 + 2.0 ** -14) * terms + base + 1e-30).all())
