@@ -223,6 +223,7 @@ __global__ void __launch_bounds__(512) balance_fwd_kernel(const BalFwdArgs a) {
 // one's shared memory.
 constexpr int BF_THREADS = 512, BF_CLUSTER = 8;
 __global__ void __launch_bounds__(BF_THREADS) balance_finish_kernel(const BalFwdArgs a) {
+    cluster_sync_all();          // the first CTA has started before anything is written to its shared memory
     pdl_begin();
     __shared__ float sh[32], share[BF_CLUSTER];
     __shared__ __align__(16) float sp[4 * BF_THREADS];
