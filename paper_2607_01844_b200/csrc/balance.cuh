@@ -23,7 +23,7 @@ namespace mop {
 struct BalSeqs { const int32_t* off; int S, T; };
 __device__ __forceinline__ int bal_off(const BalSeqs& q, int i) {
     if (!q.off) return i > 0 ? q.T : 0;
-    return min(max(__ldg(q.off + i), 0), q.T);
+    return min(max(q.off[i], 0), q.T);
 }
 // The sequence of token t: the number of offsets up to t, minus one (-1 before the first sequence, S behind the last).  A warp
 // probes 32 places at a time.
@@ -45,7 +45,7 @@ inline int bal_group(int E) { int g = 2; while (g < 32 && 4 * g < E) g *= 2; ret
 
 // Logits of this lane's experts e0 + 4 G v + q; -inf where there is none.
 template <int NV>
-__device__ __forceinline__ void bal_load(const float* __restrict__ row, const BalShape& s, int e0, bool on, float (&z)[4 * NV]) {
+__device__ __forceinline__ void bal_load(const float* row, const BalShape& s, int e0, bool on, float (&z)[4 * NV]) {
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
         const int e = e0 + 4 * s.G * v;
@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(512) balance_fwd_kernel(const BalFwdArgs a) {
             const int mine = tb + group;
             const bool on = mine < stop;
             bal_load<NV>(a.logits + (size_t)mine * s.E, s, e0, on, next);
-            pick = on && in_group < s.k ? __ldg(a.idx + (size_t)mine * s.k + in_group) : -1;
+            pick = on && in_group < s.k ? a.idx[(size_t)mine * s.k + in_group] : -1;
         };
         fetch(t + warp * tpw);
         for (int tb = t + warp * tpw; tb < stop; tb += W * tpw) {
@@ -827,7 +827,7 @@ __global__ void __launch_bounds__(256) balance_sum_kernel(const BalSumArgs a) {
 
 // The same products on the CUDA cores, for contexts whose GEMMs run there (MOP_GEMM_SCALAR).
 // dW_r = x^T dz over the tokens of the sequences; 64 x 64 outputs a block, 4 x 4 a thread.
-__global__ void __launch_bounds__(256) balance_dw_kernel(const bf16* __restrict__ x, const float* __restrict__ dz, const BalSeqs q,
+__global__ void __launch_bounds__(256) balance_dw_kernel(const bf16* x, const float* dz, const BalSeqs q,
                                                          float* __restrict__ dW, int d, int E, int accumulate) {
     pdl_begin();
     __shared__ float sx[16][64], sz[16][64];
@@ -861,7 +861,7 @@ __global__ void __launch_bounds__(256) balance_dw_kernel(const bf16* __restrict_
         }
 }
 // dX (+)= dz W_r^T, rounded to bf16 once.  Rows outside the sequences: zero, or left as they are.
-__global__ void __launch_bounds__(256) balance_dx_kernel(const float* __restrict__ dz, const float* __restrict__ W_r, const BalSeqs q,
+__global__ void __launch_bounds__(256) balance_dx_kernel(const float* dz, const float* W_r, const BalSeqs q,
                                                          bf16* __restrict__ dX, int T, int d, int E, int accumulate) {
     pdl_begin();
     __shared__ float sz[64][17], sw[64][17];

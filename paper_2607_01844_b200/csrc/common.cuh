@@ -30,6 +30,8 @@ __device__ __forceinline__ float sigmoidf_fast(float v) { return __fdividef(1.0f
 // Programmatic dependent launch: a kernel started by pdl_launch() may be brought up before its predecessor in the stream has
 // drained; pdl_begin() waits until the predecessor has finished and its writes are visible.  Nothing may be read or written
 // before it, and every kernel started by pdl_launch() calls it, or one of its two forms below, in every thread.
+// Data is read by plain loads: a read-only one (__ldg, a `const T* __restrict__` parameter) is defined only for memory that nobody writes
+// while the reader lives, and the reader may be up while the kernel before it writes.
 // A grid of few blocks also lets the next kernel come up while it runs (blocks resident, barriers and tensor memory set up).  A
 // grid that fills the SMs does not: the next kernel's blocks would pile up on the SMs that empty first (training step at
 // T 1537, d 1000, E 20: 346 us without any of this, 391 with every kernel letting its successor in at its start).

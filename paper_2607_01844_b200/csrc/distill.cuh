@@ -147,12 +147,12 @@ struct VdEntries {
         list = a.entry;
         if (on) {
             const uint16_t* f = a.first + (size_t)row * (a.units + 1);
-            const int from = __ldg(f + min(col >> 6, a.units));
-            left = (int)__ldg(f + min(end >> 6, a.units)) - from;
+            const int from = f[min(col >> 6, a.units)];
+            left = (int)f[min(end >> 6, a.units)] - from;
             list = a.entry + (size_t)row * a.K + from;
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { e[i] = make_int2(INT_MAX, 0); if (i < left) e[i] = __ldg(list + i); }
+        for (int i = 0; i < 4; ++i) { e[i] = make_int2(INT_MAX, 0); if (i < left) e[i] = list[i]; }
         list += 4;
         left -= 4;
     }
@@ -160,7 +160,7 @@ struct VdEntries {
         const int2 r = e[0];
         e[0] = e[1]; e[1] = e[2]; e[2] = e[3];
         e[3] = make_int2(INT_MAX, 0);
-        if (left > 0) { e[3] = __ldg(list); ++list; --left; }
+        if (left > 0) { e[3] = *list; ++list; --left; }
         return r;
     }
 };
@@ -222,7 +222,7 @@ struct VdScan {
             int v[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                v[i] = i0 + i < n && 32 * w + lane < K ? __ldg(base + (size_t)r * K + 32 * w + lane) : -1;
+                v[i] = i0 + i < n && 32 * w + lane < K ? base[(size_t)r * K + 32 * w + lane] : -1;
                 if (++w == words) { w = 0; ++r; }
             }
 #pragma unroll
@@ -253,7 +253,7 @@ struct VdScan {
         for (int k0 = 0; k0 < K; k0 += 8) {
             int v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = k0 + i < K ? __ldg(list + k0 + i) : -1;
+            for (int i = 0; i < 8; ++i) v[i] = k0 + i < K ? list[k0 + i] : -1;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (v[i] >= col && v[i] < end && ++seen > 8) f(v[i] - col, k0 + i);
@@ -510,8 +510,8 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
                 if constexpr (KIND == VD_R) {
                     if (mine) coef = args.row_scale[row];
 #pragma unroll
-                    for (int g = 0; g < 4; ++g) scale[g] = __ldg(args.col_scale + col0 / 32 + g);
-                    if (args.add_to && args.seq_off) inside = row >= __ldg(args.seq_off) && row < __ldg(args.seq_off + args.n_seq);
+                    for (int g = 0; g < 4; ++g) scale[g] = args.col_scale[col0 / 32 + g];
+                    if (args.add_to && args.seq_off) inside = row >= args.seq_off[0] && row < args.seq_off[args.n_seq];
                 }
                 VdEntries en;
                 (void)en;
@@ -881,7 +881,7 @@ __global__ void __launch_bounds__(DM_THREADS) distill_merge_kernel(const Distill
 
 // dX from its fp32 sums [splits, N, pitch], four elements a thread; with many ranges (few tokens, hence few elements) four lanes share
 // them, each adds every fourth range, and their sums are added in order (N 4, H 576, 64 ranges: 22 us by single threads, 7 by four).
-__global__ void __launch_bounds__(256) distill_dx_kernel(const float* __restrict__ src, bf16* __restrict__ dst, int N, int H, int pitch,
+__global__ void __launch_bounds__(256) distill_dx_kernel(const float* src, bf16* __restrict__ dst, int N, int H, int pitch,
                                                          int splits) {
     pdl_begin();
     const int per = H / 4, lanes = splits >= 8 ? 4 : 1, sub = threadIdx.x % lanes, elements = 256 / lanes;

@@ -31,3 +31,15 @@ def test_another_ctas_shared_memory_is_used_only_after_a_cluster_barrier(path):
         if "__global__" in body:
             uses = [m.start() for r in remote for m in re.finditer(r, body)]
             assert not uses or "cluster_sync_all()" in body[:min(uses)], body[:160]
+
+
+LAUNCHED_EARLY = [CSRC / "balance.cuh", CSRC / "distill.cuh"]
+
+
+@pytest.mark.parametrize("path", LAUNCHED_EARLY, ids=lambda p: p.name)
+def test_nothing_is_read_through_the_read_only_path(path):
+    """A kernel that programmatic launches bring up early lives while the one before it still writes, and a read-only load (__ldg, or a
+    kernel's `const ... * __restrict__` parameter, which the compiler may turn into one) is defined only for memory that nobody writes
+    in the reader's lifetime; nor does the compiler have to keep such a load behind the wait for the grid before."""
+    text = code(path)
+    assert "__ldg" not in text and "ld.global.nc" not in text and not re.search(r"const\s+\w+\s*\*\s*__restrict__", text)
