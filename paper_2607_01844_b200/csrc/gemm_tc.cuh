@@ -403,13 +403,13 @@ __device__ __forceinline__ TileInfo decode_tile(const TcArgs& a, int t) {
             const int half_n = a.tiles_n >> 1;
             if (ti.nt >= half_n) { ti.nt -= half_n; ti.sel = 1; }
         }
-        ti.row0 = __ldg(a.offsets + ti.e);
-        ti.rows = __ldg(a.offsets + ti.e + 1) - ti.row0;
+        ti.row0 = a.offsets[ti.e];
+        ti.rows = a.offsets[ti.e + 1] - ti.row0;
         ti.skip = ti.rows <= 0;
     } else {
         int mt, nt;
         mt = t / a.tiles_n; nt = t - mt * a.tiles_n;
-        const int4 m = __ldg(a.mtiles + mt);
+        const int4 m = a.mtiles[mt];
         ti.e = m.x; ti.row0 = m.y; ti.rows = m.z; ti.m0 = 0;
         ti.nt = nt;
         ti.skip = false;
@@ -418,7 +418,7 @@ __device__ __forceinline__ TileInfo decode_tile(const TcArgs& a, int t) {
 }
 
 // 128-row tile list of the ragged-M GEMMs, built on the device from offsets (no host round trip).
-__device__ __forceinline__ void tc_build_mtiles_body(const int32_t* __restrict__ offsets, int E,
+__device__ __forceinline__ void tc_build_mtiles_body(const int32_t* offsets, int E,
                                                      int4* __restrict__ mtiles, int32_t* __restrict__ n_mtiles,
                                                      int32_t* scan) {
     const int e = threadIdx.x;
@@ -438,7 +438,7 @@ __device__ __forceinline__ void tc_build_mtiles_body(const int32_t* __restrict__
     for (int i = 0; i < nt; ++i) mtiles[first + i] = make_int4(e, off + i * TC_BM, min(TC_BM, cnt - i * TC_BM), 0);
     if (e == 1023) *n_mtiles = scan[1023];
 }
-__global__ void __launch_bounds__(1024) tc_build_mtiles_kernel(const int32_t* __restrict__ offsets, int E,
+__global__ void __launch_bounds__(1024) tc_build_mtiles_kernel(const int32_t* offsets, int E,
                                                                int4* __restrict__ mtiles,
                                                                int32_t* __restrict__ n_mtiles) {
     pdl_begin();
@@ -619,7 +619,7 @@ tc_grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_co
         // the next tile's descriptor is fetched one tile ahead so that its latency is hidden
         TileInfo nxt = decode_tile<KIND>(args, min((int)blockIdx.x, max(total_tiles - 1, 0)));
         int expert = -1, ahead = 0;
-        const int rows_total = Tr::RAGGED_K ? __ldg(args.offsets + args.E) : 0;
+        const int rows_total = Tr::RAGGED_K ? args.offsets[args.E] : 0;
         (void)expert; (void)ahead; (void)rows_total;
         for (int t = blockIdx.x; t < total_tiles && alive; t += gridDim.x) {
             const TileInfo ti = nxt;
@@ -884,7 +884,7 @@ tc_grouped_gemm_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_co
 // logit minus lse.  A block owns 32 rows (a lane each) and its eight warps every eighth tile; the eight results are merged in
 // order: reproducible.  (One thread per row and all tiles: 19 us at 2048 rows, 125 tiles.)
 constexpr int LSE_WARPS = 8;
-__global__ void __launch_bounds__(32 * LSE_WARPS) vocab_lse_merge_kernel(const float2* __restrict__ part, const float* __restrict__ ylab,
+__global__ void __launch_bounds__(32 * LSE_WARPS) vocab_lse_merge_kernel(const float2* part, const float* ylab,
                                                                          float* __restrict__ loss, float* __restrict__ lse, int N,
                                                                          int ntiles) {
     pdl_begin();
@@ -927,7 +927,7 @@ __global__ void __launch_bounds__(256) vocab_setup_kernel(int N, int4* __restric
 }
 
 // fp32 -> bf16 of a dense array (8 elements per thread; n a multiple of 8)
-__global__ void f32_to_bf16_kernel(const float4* __restrict__ src, uint4* __restrict__ dst, size_t n8) {
+__global__ void f32_to_bf16_kernel(const float4* src, uint4* __restrict__ dst, size_t n8) {
     pdl_begin();
     for (size_t i = blockIdx.x * (size_t)blockDim.x + threadIdx.x; i < n8; i += (size_t)gridDim.x * blockDim.x) {
         const float4 a = src[2 * i], b = src[2 * i + 1];

@@ -114,7 +114,7 @@ __host__ __device__ constexpr uint32_t make_idesc2(bool a_mn, bool b_mn) {
 }
 
 // 256-row pair tiles of the ragged-M GEMMs: {expert, first row, rows in the pair (1..256), 0}.
-__global__ void __launch_bounds__(1024) tc_build_pairtiles_kernel(const int32_t* __restrict__ offsets, int E,
+__global__ void __launch_bounds__(1024) tc_build_pairtiles_kernel(const int32_t* offsets, int E,
                                                                   int4* __restrict__ tiles,
                                                                   int32_t* __restrict__ n_tiles) {
     __shared__ int32_t scan[1025];
@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(1024) tc_build_pairtiles_kernel(const int32_t*
 // Mixed schedule: the full 256-row pairs of every expert go to the two-CTA kernel, the remaining
 // rows (< 256 per expert, as one or two 128-row tiles) to the one-CTA kernel, so that pairing adds
 // no padding.  One launch builds both lists.
-__global__ void __launch_bounds__(1024) tc_build_mixed_kernel(const int32_t* __restrict__ offsets, int E,
+__global__ void __launch_bounds__(1024) tc_build_mixed_kernel(const int32_t* offsets, int E,
                                                               int4* __restrict__ pair_tiles,
                                                               int32_t* __restrict__ n_pairs,
                                                               int4* __restrict__ single_tiles,
@@ -226,7 +226,7 @@ tc_gemm2_kernel(const __grid_constant__ CUtensorMap tmA0, const __grid_constant_
         } else { mt = t / args.tiles_n; nt = t - mt * args.tiles_n; }
         int4 m;
         if constexpr (KIND == TC_VW) m = make_int4(0, 256 * mt, min(256, args.Mfix - 256 * mt), 0);
-        else m = __ldg(args.mtiles + mt);
+        else m = args.mtiles[mt];
         ti.e = m.x; ti.row0 = m.y + 128 * (int)rank; ti.rows = min(128, max(0, m.z - 128 * (int)rank));
         ti.m0 = 0; ti.nt = nt; ti.skip = false;
         return ti;

@@ -88,7 +88,7 @@ struct TnArgs {
 
 // The tile tables of the token-row GEMMs in one launch: block 0 the token tiles, block 1 the 128-row tiles of the
 // tokens-on-M kernels (where a forward or backward uses both).
-__global__ void __launch_bounds__(1024) tn_build_ttiles_kernel(const int32_t* __restrict__ offsets, int E, int32_t* __restrict__ ttiles,
+__global__ void __launch_bounds__(1024) tn_build_ttiles_kernel(const int32_t* offsets, int E, int32_t* __restrict__ ttiles,
                                                                int32_t* __restrict__ mtiles) {
     pdl_begin();
     __shared__ int32_t scan[1025];
@@ -335,14 +335,14 @@ tn_gemm_kernel(const __grid_constant__ TnMaps maps, const TnArgs args) {
     auto decode = [&](int t) {
         if (t >= total_tiles) return make_int4(-1, 0, 0, 0);
         const int q = t / args.tiles_m;
-        int4 m = __ldg(args.ttiles + q);
+        int4 m = args.ttiles[q];
         const int nt = m.w >> 16;
         int mt = t - q * args.tiles_m;
         if (nt > 1) {
             const int first = q - (m.w & 0xffff);                 // first token tile of this expert
             const int l = t - first * args.tiles_m;               // position among the expert's work items
             mt = l / nt;
-            m = __ldg(args.ttiles + first + (l - mt * nt));
+            m = args.ttiles[first + (l - mt * nt)];
         }
         return make_int4(m.x, m.y, m.z, mt);
     };
@@ -372,7 +372,7 @@ tn_gemm_kernel(const __grid_constant__ TnMaps maps, const TnArgs args) {
             int tok[4] = {0, 0, 0, 0};
             if (lane < ngroups) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) tok[j] = __ldg(args.row_src + min(brow0 + 4 * lane + j, last)) / args.topk;
+                for (int j = 0; j < 4; ++j) tok[j] = args.row_src[min(brow0 + 4 * lane + j, last)] / args.topk;
             }
             const uint32_t tx = 2u * (TN_SUB_BYTES + (uint32_t)half * 128u);
             for (int kb = 0; kb < args.kblocks; ++kb) {

@@ -84,8 +84,8 @@ tw_wgrad_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
             const int half_n = args.tiles_n >> 1;
             if (ti.nt >= half_n) { ti.nt -= half_n; ti.sel = 1; }
         }
-        ti.row0 = __ldg(args.offsets + ti.e);
-        ti.rows = __ldg(args.offsets + ti.e + 1) - ti.row0;
+        ti.row0 = args.offsets[ti.e];
+        ti.rows = args.offsets[ti.e + 1] - ti.row0;
         ti.skip = ti.rows <= 0;
         return ti;
     };
@@ -110,7 +110,7 @@ tw_wgrad_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__
         const uint64_t keep = l2_policy_evict_last();
         TileInfo nxt = decode(min(cluster_id, max(total_tiles - 1, 0)));
         int expert = -1, ahead = 0;
-        const int rows_total = __ldg(args.offsets + args.E);
+        const int rows_total = args.offsets[args.E];
         for (int t = cluster_id; t < total_tiles && alive; t += n_clusters) {
             const TileInfo ti = nxt;
             if (t + n_clusters < total_tiles) nxt = decode(t + n_clusters);

@@ -10,7 +10,7 @@ constexpr int PERM_SEG = 512;    // assignments walked by one warp ("unit")
 constexpr int PERM_WARPS = 4;    // warps per block in the histogram / rank kernels
 
 // Histogram per unit: partial[u][e] = number of assignments of unit u that go to expert e.
-__global__ void __launch_bounds__(PERM_WARPS * 32) perm_hist_kernel(const int32_t* __restrict__ idx,
+__global__ void __launch_bounds__(PERM_WARPS * 32) perm_hist_kernel(const int32_t* idx,
                                                                     int32_t* __restrict__ partial, int M, int E) {
     pdl_begin();
     extern __shared__ int32_t perm_smem[];
@@ -113,9 +113,9 @@ __global__ void __launch_bounds__(PSCAN_WARPS * 32) perm_scan_cols_kernel(int32_
 // Rank: second walk over the same segments; perm_row[a] = offsets[e] + base[u][e] + rank inside the unit.
 // Every block scans counts[] into the experts' offsets for itself (E <= 1024 words of shared memory);
 // block 0 also writes them out.
-__global__ void __launch_bounds__(PERM_WARPS * 32) perm_rank_kernel(const int32_t* __restrict__ idx,
-                                                                    const int32_t* __restrict__ base,
-                                                                    const int32_t* __restrict__ counts,
+__global__ void __launch_bounds__(PERM_WARPS * 32) perm_rank_kernel(const int32_t* idx,
+                                                                    const int32_t* base,
+                                                                    const int32_t* counts,
                                                                     int32_t* __restrict__ offsets,
                                                                     int32_t* __restrict__ perm_row,
                                                                     int32_t* __restrict__ row_src, int M, int E) {
@@ -242,7 +242,7 @@ __device__ __forceinline__ void perm_cluster_scan(const PermSmem& sm, int32_t* _
     __syncthreads();
 }
 
-__global__ void __launch_bounds__(PC_WARPS * 32) perm_cluster_kernel(const int32_t* __restrict__ idx, int32_t* __restrict__ counts,
+__global__ void __launch_bounds__(PC_WARPS * 32) perm_cluster_kernel(const int32_t* idx, int32_t* __restrict__ counts,
                                                                      int32_t* __restrict__ offsets, int32_t* __restrict__ perm_row,
                                                                      int32_t* __restrict__ row_src, int M, int E, int per_warp,
                                                                      int32_t* __restrict__ tile_table) {
@@ -318,8 +318,8 @@ inline void launch_perm_cluster(const int32_t* idx, int32_t* counts, int32_t* of
 
 // Scatter rows: one warp per token reads x[t,:] once (16-byte vectors, coalesced) and writes it to
 // its k destination rows.  Used for x -> Xp and for dY -> dYp.
-__global__ void __launch_bounds__(256) scatter_rows_kernel(const uint4* __restrict__ src, uint4* __restrict__ dst,
-                                                           const int32_t* __restrict__ perm_row, int T, int k,
+__global__ void __launch_bounds__(256) scatter_rows_kernel(const uint4* src, uint4* __restrict__ dst,
+                                                           const int32_t* perm_row, int T, int k,
                                                            int vec_per_row, TileJob job) {
     pdl_begin();
     if (tile_block(job)) return;
@@ -334,7 +334,7 @@ __global__ void __launch_bounds__(256) scatter_rows_kernel(const uint4* __restri
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const int c = c0 + q * 32 + lane;
-                if (c < vec_per_row) v[q] = __ldg(s + c);
+                if (c < vec_per_row) v[q] = s[c];
             }
             for (int j = 0; j < k; ++j) {
                 const int32_t p = __shfl_sync(0xffffffffu, myrow, j);
@@ -354,8 +354,8 @@ __global__ void __launch_bounds__(256) scatter_rows_kernel(const uint4* __restri
 // bytes): the row is read once and each of its k copies is written as one contiguous run, which DRAM takes
 // better than pieces of 2 KiB interleaved over k rows (random 2 KiB pieces: 4.4 TB/s at T = 16384, d = 7168).
 template <int VPL>
-__global__ void __launch_bounds__(256) scatter_rows_reg_kernel(const uint4* __restrict__ src, uint4* __restrict__ dst,
-                                                               const int32_t* __restrict__ perm_row, int T, int k,
+__global__ void __launch_bounds__(256) scatter_rows_reg_kernel(const uint4* src, uint4* __restrict__ dst,
+                                                               const int32_t* perm_row, int T, int k,
                                                                int vec_per_row, TileJob job) {
     pdl_begin();
     if (tile_block(job)) return;
@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(256) scatter_rows_reg_kernel(const uint4* __re
 #pragma unroll
         for (int q = 0; q < VPL; ++q) {
             const int c = q * 32 + lane;
-            if (c < vec_per_row) v[q] = __ldg(s + c);
+            if (c < vec_per_row) v[q] = s[c];
         }
         for (int j = 0; j < k; ++j) {
             const int32_t p = __shfl_sync(0xffffffffu, myrow, j);
@@ -396,7 +396,7 @@ __device__ __forceinline__ uint4 pack_bf16x8(const float (&a)[8]) {
 // the copy rate), and there one row of 2 KiB at a time does best (T = 8192, d = 4096, k = 4: 55 us, 64 with two rows of 1 KiB, 78 with
 // four, 82 with a warp per token and rows of 4 KiB).
 constexpr int COMB_SEG = 4;
-__global__ void __launch_bounds__(256) combine_rows_kernel(const uint4* __restrict__ Yp, const int32_t* __restrict__ perm_row,
+__global__ void __launch_bounds__(256) combine_rows_kernel(const uint4* Yp, const int32_t* perm_row,
                                                             uint4* __restrict__ Y, int T, int k, int vec_per_row) {
     pdl_begin();
     const int lane = threadIdx.x % 32;
@@ -430,7 +430,7 @@ __global__ void __launch_bounds__(256) combine_rows_kernel(const uint4* __restri
 // Little to do, or rows too short for that: a thread per vector of Y, R of its rows in flight.  Nothing is left idle where a row is
 // no multiple of what a warp takes, and there is little to set up.
 template <int R>
-__global__ void __launch_bounds__(256) combine_vectors_kernel(const uint4* __restrict__ Yp, const int32_t* __restrict__ perm_row,
+__global__ void __launch_bounds__(256) combine_vectors_kernel(const uint4* Yp, const int32_t* perm_row,
                                                               uint4* __restrict__ Y, uint32_t n, int k, uint32_t vec_per_row) {
     pdl_begin();
     for (uint32_t i = blockIdx.x * blockDim.x + threadIdx.x; i < n; i += gridDim.x * blockDim.x) {
@@ -492,7 +492,7 @@ inline void launch_combine_rows(const uint4* Yp, const int32_t* perm_row, uint4*
 
 // dgate[a] = sum over n-tiles of the partial dot products written by the dgrad-down epilogue
 // (row p = perm_row[a]; fixed order, so the result is reproducible).
-__global__ void dgate_reduce_kernel(const float* __restrict__ part, const int32_t* __restrict__ perm_row,
+__global__ void dgate_reduce_kernel(const float* part, const int32_t* perm_row,
                                     float* __restrict__ dgate, int M, int ntiles) {
     pdl_begin();
     const int a = blockIdx.x * blockDim.x + threadIdx.x;
@@ -513,9 +513,9 @@ __global__ void dgate_reduce_kernel(const float* __restrict__ part, const int32_
 // Tables of one chunk: off_c[e] = first row of expert e inside the chunk's buffers (experts outside the
 // chunk get no rows), row_src_c[r] = assignment of chunk row r, perm_c[a] = chunk row of assignment a or -1.
 // bounds[0] = first row of the chunk in the whole layer, bounds[1] = its rows.
-__global__ void __launch_bounds__(256) chunk_tables_kernel(const int32_t* __restrict__ offsets,
-                                                           const int32_t* __restrict__ row_src,
-                                                           const int32_t* __restrict__ perm_row,
+__global__ void __launch_bounds__(256) chunk_tables_kernel(const int32_t* offsets,
+                                                           const int32_t* row_src,
+                                                           const int32_t* perm_row,
                                                            int32_t* __restrict__ off_c, int32_t* __restrict__ row_src_c,
                                                            int32_t* __restrict__ perm_c, int32_t* __restrict__ bounds,
                                                            int E, int M, int chunk, int n_chunks) {
@@ -549,9 +549,9 @@ constexpr int CHUNK_SEG = 4;
 
 // Xp_c[r,:] = x[row_src_c[r] / k, :] for the rows of a chunk (16-byte vectors).
 // d = 7168, 4096 rows (117 MB): 25 us, 26 with a warp per row.
-__global__ void __launch_bounds__(256) gather_rows_kernel(const uint4* __restrict__ src, uint4* __restrict__ dst,
-                                                          const int32_t* __restrict__ row_src_c,
-                                                          const int32_t* __restrict__ bounds, int k, int vec_per_row,
+__global__ void __launch_bounds__(256) gather_rows_kernel(const uint4* src, uint4* __restrict__ dst,
+                                                          const int32_t* row_src_c,
+                                                          const int32_t* bounds, int k, int vec_per_row,
                                                           TileJob job) {
     pdl_begin();
     if (tile_block(job)) return;
@@ -565,7 +565,7 @@ __global__ void __launch_bounds__(256) gather_rows_kernel(const uint4* __restric
         uint4 v[CHUNK_SEG];
 #pragma unroll
         for (int u = 0; u < CHUNK_SEG; ++u)
-            if (c + 32 * u < vec_per_row) v[u] = __ldg(s + c + 32 * u);
+            if (c + 32 * u < vec_per_row) v[u] = s[c + 32 * u];
 #pragma unroll
         for (int u = 0; u < CHUNK_SEG; ++u)
             if (c + 32 * u < vec_per_row) __stcs(o + c + 32 * u, v[u]);
@@ -577,8 +577,8 @@ __global__ void __launch_bounds__(256) gather_rows_kernel(const uint4* __restric
 // written, not read; last: the sum is rounded once to bf16 into out instead of going back to acc.
 // d = 7168, 4096 tokens, 4 chunks of 4096 rows (about 225 MB for one in the middle): 47 us, 93 with a warp per
 // row; 2 or 7 vectors a lane instead of 4: 47 and 50.
-__global__ void __launch_bounds__(256) combine_acc_kernel(const uint4* __restrict__ Yp_c,
-                                                          const int32_t* __restrict__ perm_c, float4* __restrict__ acc,
+__global__ void __launch_bounds__(256) combine_acc_kernel(const uint4* Yp_c,
+                                                          const int32_t* perm_c, float4* __restrict__ acc,
                                                           uint4* __restrict__ out, int T, int k, int vec_per_row,
                                                           int first, int last) {
     pdl_begin();
@@ -628,7 +628,7 @@ __global__ void __launch_bounds__(256) combine_acc_kernel(const uint4* __restric
 }
 
 // dgate of the assignments that lie inside the chunk (others are left alone).
-__global__ void dgate_reduce_chunk_kernel(const float* __restrict__ part, const int32_t* __restrict__ perm_c,
+__global__ void dgate_reduce_chunk_kernel(const float* part, const int32_t* perm_c,
                                           float* __restrict__ dgate, int M, int rows_pitch, int ntiles) {
     pdl_begin();
     const int a = blockIdx.x * blockDim.x + threadIdx.x;
@@ -641,7 +641,7 @@ __global__ void dgate_reduce_chunk_kernel(const float* __restrict__ part, const 
 }
 
 // Zero the weight gradients of the experts that received no row (the chunked backward writes only experts with rows).
-__global__ void __launch_bounds__(256) zero_empty_experts_kernel(const int32_t* __restrict__ offsets,
+__global__ void __launch_bounds__(256) zero_empty_experts_kernel(const int32_t* offsets,
                                                                 float4* __restrict__ dWg, float4* __restrict__ dWu,
                                                                 float4* __restrict__ dWd, size_t vec_per_expert) {
     pdl_begin();

@@ -42,7 +42,7 @@ __device__ __forceinline__ uint32_t order_key(float v) {
 
 // Q = E / 32 rounded up, or more.  On return lane j < k holds the j-th pick and its gate.
 template <int Q>
-__device__ __forceinline__ void select_token(const float* __restrict__ z, const float* __restrict__ bias, int E, int k,
+__device__ __forceinline__ void select_token(const float* z, const float* bias, int E, int k,
                                              int score_fn, int bias_mode, int lane, int& my_e, float& my_gate) {
     // The loads of a lane first, all in flight: with the forms of the key inside one loop each load waited for the branch of the one
     // before it (router at T 64, d 64, k 1: E 1024 15.7 us, now 4.2; E 256 5.7 and 3.4; T 16384, E 256, k 8 with a bias 53 and 40).
@@ -100,7 +100,7 @@ __device__ __forceinline__ void select_token(const float* __restrict__ z, const 
 }
 
 template <int Q>
-__global__ void __launch_bounds__(SEL_WARPS * 32) route_select_kernel(const float* __restrict__ z, const float* __restrict__ bias,
+__global__ void __launch_bounds__(SEL_WARPS * 32) route_select_kernel(const float* z, const float* bias,
                                                                       int32_t* __restrict__ idx, float* __restrict__ gate, int T,
                                                                       int E, int k, int score_fn, int bias_mode) {
     pdl_begin();
@@ -161,7 +161,7 @@ inline void launch_route_select(const float* z, const float* bias, int32_t* idx,
 
 // W_r [d,E] -> three bf16 pieces [3,d,E], the transposed copy W_r^T [E,d] (32 x 32 tiles through shared
 // memory) and, per 32-row slab, the partial squared column norms (summed by route_wnorm_kernel).
-__global__ void __launch_bounds__(256) route_prep_kernel(const float* __restrict__ W_r, bf16* __restrict__ pieces,
+__global__ void __launch_bounds__(256) route_prep_kernel(const float* W_r, bf16* __restrict__ pieces,
                                                          float* __restrict__ W_rT, float* __restrict__ colsq,
                                                          int d, int E) {
     __shared__ float tile[32][33];
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(256) route_prep_kernel(const float* __restrict
 }
 
 // Squared column norms ||W_r[:,e]||^2 from the slab partials: one warp per expert, fixed order (reproducible).
-__global__ void __launch_bounds__(256) route_wnorm_kernel(const float* __restrict__ colsq, float* __restrict__ wsq,
+__global__ void __launch_bounds__(256) route_wnorm_kernel(const float* colsq, float* __restrict__ wsq,
                                                           int slabs, int E) {
     const int lane = threadIdx.x % 32;
     const int e = blockIdx.x * 8 + threadIdx.x / 32;
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(256) route_wnorm_kernel(const float* __restric
 }
 
 // ||x_t||_2 per token: one warp per row, 16-byte loads.
-__global__ void __launch_bounds__(256) route_xnorm_kernel(const bf16* __restrict__ x, float* __restrict__ xnorm, int T,
+__global__ void __launch_bounds__(256) route_xnorm_kernel(const bf16* x, float* __restrict__ xnorm, int T,
                                                           int d) {
     const int lane = threadIdx.x % 32;
     const int t = blockIdx.x * 8 + threadIdx.x / 32;
@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(256) route_xnorm_kernel(const bf16* __restrict
     const uint4* row = reinterpret_cast<const uint4*>(x + (size_t)t * d);
     float sq = 0.0f;
     for (int v = lane; v < d / 8; v += 32) {
-        const uint4 q = __ldg(row + v);
+        const uint4 q = row[v];
         const uint32_t w4[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -301,10 +301,10 @@ __device__ __forceinline__ float key_error(float zz, float ez, int score_fn, int
 // pair_cnt [E], pair_list [E][T]: tokens listed per expert; pre [T][32]: bit q of word l: expert l + 32 q was listed.
 template <bool RESOLVE, int Q>
 __device__ __forceinline__ bool route_token(int t, int lane, float* zg, int32_t* clist, float* xs, float* ws,
-                                            float* __restrict__ z, const float* __restrict__ z1,
-                                            const float* __restrict__ bias,
-                                            const bf16* __restrict__ x, const float* __restrict__ W_rT,
-                                            const float* __restrict__ xnorm, float wmax, int32_t* __restrict__ idx,
+                                            float* __restrict__ z, const float* z1,
+                                            const float* bias,
+                                            const bf16* x, const float* W_rT,
+                                            const float* xnorm, float wmax, int32_t* __restrict__ idx,
                                             float* __restrict__ gate, int32_t* __restrict__ stats,
                                             int32_t* __restrict__ pair_cnt, int32_t* __restrict__ pair_list,
                                             uint32_t* __restrict__ pre, int T, int d, int E, int k, int score_fn,
@@ -423,12 +423,12 @@ __device__ __forceinline__ bool route_token(int t, int lane, float* zg, int32_t*
 #pragma unroll
                 for (int u = 0; u < XV; ++u)
                     if (lane + 32 * u < n / 8)
-                        xq[u] = __ldg(reinterpret_cast<const uint4*>(x + (size_t)t * d + i0) + lane + 32 * u);
+                        xq[u] = *(reinterpret_cast<const uint4*>(x + (size_t)t * d + i0) + lane + 32 * u);
 #pragma unroll
                 for (int u = 0; u < WV; ++u) {
                     const int v = lane + 32 * u, c = v / (SELF_XCHUNK / 4), j = v % (SELF_XCHUNK / 4);
                     if (c < nc && 4 * j < n)
-                        wq[u] = __ldg(reinterpret_cast<const float4*>(W_rT + (size_t)clist[c0 + c] * d + i0) + j);
+                        wq[u] = *(reinterpret_cast<const float4*>(W_rT + (size_t)clist[c0 + c] * d + i0) + j);
                 }
             };
             fetch(0);
@@ -515,7 +515,7 @@ __device__ __forceinline__ bool route_token(int t, int lane, float* zg, int32_t*
 }
 
 // Largest column norm of W_r, from the squared norms: every lane returns it.
-__device__ __forceinline__ float route_wmax(const float* __restrict__ wsq, int E, int lane) {
+__device__ __forceinline__ float route_wmax(const float* wsq, int E, int lane) {
     float wmax2 = 0.0f;
     for (int e = lane; e < E; e += 32) wmax2 = fmaxf(wmax2, wsq[e]);
 #pragma unroll
@@ -529,8 +529,8 @@ __device__ __forceinline__ float route_wmax(const float* __restrict__ wsq, int E
 constexpr int SCREEN_WARPS = 4;
 template <int Q>
 __global__ void __launch_bounds__(SCREEN_WARPS * 32) route_screen_kernel(
-    float* __restrict__ z, const float* __restrict__ z1, const float* __restrict__ bias,
-    const float* __restrict__ xnorm, const float* __restrict__ wsq, int32_t* __restrict__ idx, float* __restrict__ gate,
+    float* __restrict__ z, const float* z1, const float* bias,
+    const float* xnorm, const float* wsq, int32_t* __restrict__ idx, float* __restrict__ gate,
     int32_t* __restrict__ todo, int32_t* __restrict__ n_todo, int32_t* __restrict__ pair_cnt,
     int32_t* __restrict__ pair_list, uint32_t* __restrict__ pre, int T, int d, int E, int k, int score_fn, int bias_mode) {
     extern __shared__ float sel_smem[];
@@ -566,8 +566,8 @@ constexpr int CHAIN_STAGE_BYTES = 32 * CHAIN_XPITCH + CHAIN_K * 4;
 constexpr int CHAIN_SMEM_BYTES = CHAIN_WARPS * CHAIN_STAGES * CHAIN_STAGE_BYTES;
 constexpr int CHAIN_BLOCKS = 227 * 1024 / (CHAIN_SMEM_BYTES + 6144);     // resident per SM
 __global__ void __launch_bounds__(CHAIN_WARPS * 32) route_chain_kernel(
-    float* __restrict__ z, const bf16* __restrict__ x, const float* __restrict__ W_rT, const float* __restrict__ xnorm,
-    const float* __restrict__ wsq, const int32_t* __restrict__ pair_cnt, const int32_t* __restrict__ pair_list,
+    float* __restrict__ z, const bf16* x, const float* W_rT, const float* xnorm,
+    const float* wsq, const int32_t* pair_cnt, const int32_t* pair_list,
     int32_t* __restrict__ stats, int min_listed, int T, int d, int E) {
     pdl_begin();
     extern __shared__ __align__(16) char chain_smem[];
@@ -677,9 +677,9 @@ inline bool route_chain_init() {
 // Resolving pass: the listed tokens, one warp each, with the staging memory of the chains.
 template <int Q>
 __global__ void __launch_bounds__(SELF_WARPS * 32) route_resolve_kernel(
-    float* __restrict__ z, const float* __restrict__ bias, const bf16* __restrict__ x, const float* __restrict__ W_rT,
-    const float* __restrict__ xnorm, const float* __restrict__ wsq, int32_t* __restrict__ idx,
-    float* __restrict__ gate, const int32_t* __restrict__ todo, const int32_t* __restrict__ n_todo,
+    float* __restrict__ z, const float* bias, const bf16* x, const float* W_rT,
+    const float* xnorm, const float* wsq, int32_t* __restrict__ idx,
+    float* __restrict__ gate, const int32_t* todo, const int32_t* n_todo,
     int32_t* __restrict__ stats, uint32_t* __restrict__ pre, int min_listed, int d, int E, int k, int score_fn, int bias_mode) {
     pdl_begin();
     extern __shared__ float sel_smem[];
@@ -769,7 +769,7 @@ inline void route_select_fast(float* z, const float* z1, const float* bias, cons
 // ---------------------------------------------------------------------------------------------
 
 // W_r^T [E,d] from W_r [d,E], a tile of 32 x 32 per block through shared memory: gives the dX kernel contiguous rows.
-__device__ __forceinline__ void transpose_tile(const float* __restrict__ in, float* __restrict__ out, int rows, int cols, int block) {
+__device__ __forceinline__ void transpose_tile(const float* in, float* __restrict__ out, int rows, int cols, int block) {
     __shared__ float tile[32][33];
     const int across = (cols + 31) / 32;
     const int c0 = (block % across) * 32, r0 = (block / across) * 32;
@@ -784,15 +784,15 @@ __device__ __forceinline__ void transpose_tile(const float* __restrict__ in, flo
 // One warp per token: lane j < k owns the j-th selected expert.  Writes dz per assignment and, in
 // expert-contiguous row order (row = perm_row[assignment]), the copy that the dW_r kernel reads.
 // The blocks behind the first dz_blocks transpose W_r, which the next kernel reads as well: a launch less.
-__global__ void __launch_bounds__(256) route_bwd_dz_kernel(const float* __restrict__ logits,
-                                                           const float* __restrict__ bias,
-                                                           const int32_t* __restrict__ idx,
-                                                           const float* __restrict__ gate,
-                                                           const float* __restrict__ dgate,
-                                                           const int32_t* __restrict__ perm_row,
+__global__ void __launch_bounds__(256) route_bwd_dz_kernel(const float* logits,
+                                                           const float* bias,
+                                                           const int32_t* idx,
+                                                           const float* gate,
+                                                           const float* dgate,
+                                                           const int32_t* perm_row,
                                                            float* __restrict__ dz_sel, float* __restrict__ dz_row,
                                                            int T, int E, int k, int score_fn, int bias_mode, int dz_blocks,
-                                                           const float* __restrict__ W_r, float* __restrict__ W_rT, int d) {
+                                                           const float* W_r, float* __restrict__ W_rT, int d) {
     pdl_begin();
     if ((int)blockIdx.x >= dz_blocks) { transpose_tile(W_r, W_rT, d, E, blockIdx.x - dz_blocks); return; }
     const int lane = threadIdx.x % 32;
@@ -833,8 +833,8 @@ __global__ void __launch_bounds__(256) route_bwd_dz_kernel(const float* __restri
 // time; dX is read, updated in fp32 and rounded back to bf16.  d is a multiple of 8.
 // Bound by what the rows of W_r^T cost: k fp32 columns for each bf16 one of dX.  With the columns fixed, E KiB of them pass through an
 // SM's L1 again and again, instead of all E rows through L2.
-__device__ __forceinline__ void route_bwd_dx(const float* __restrict__ W_rT, const int32_t* __restrict__ idx,
-                                             const float* __restrict__ dz_sel, bf16* __restrict__ dX, int T, int d, int k, int block,
+__device__ __forceinline__ void route_bwd_dx(const float* W_rT, const int32_t* idx,
+                                             const float* dz_sel, bf16* __restrict__ dX, int T, int d, int k, int block,
                                              int blocks) {
     const int lane = threadIdx.x % 32, warps = blockDim.x / 32, segs = (d + 255) / 256;
     const int i = (block % segs) * 256 + lane * 4;
@@ -892,10 +892,10 @@ __device__ __forceinline__ void route_bwd_dx(const float* __restrict__ W_rT, con
 // there were too few bytes in flight: 141 us at T = 4096, d = 2048, E = 64, k = 6 and 292 us at T = 4096, d = 1024, E = 32,
 // k = 8; now 28 and 21.  Fixed order, no atomics.
 // The blocks behind these, if any, add the router's share to dX: neither waits for the other.
-__global__ void __launch_bounds__(1024) route_bwd_dwr_dx_kernel(const bf16* __restrict__ Xp, const float* __restrict__ dz_row,
-                                                                const int32_t* __restrict__ offsets, float* __restrict__ dW_r,
-                                                                float* __restrict__ dbias, int d, int E, const float* __restrict__ W_rT,
-                                                                const int32_t* __restrict__ idx, const float* __restrict__ dz_sel,
+__global__ void __launch_bounds__(1024) route_bwd_dwr_dx_kernel(const bf16* Xp, const float* dz_row,
+                                                                const int32_t* offsets, float* __restrict__ dW_r,
+                                                                float* __restrict__ dbias, int d, int E, const float* W_rT,
+                                                                const int32_t* idx, const float* dz_sel,
                                                                 bf16* __restrict__ dX, int T, int k) {
     pdl_begin();
     extern __shared__ float dwr_smem[];                              // [W][256]

@@ -17,10 +17,10 @@ constexpr long long RP_MAX_BYTES = 1 << 20;        // of the copied rows
 
 template <int Q>
 __global__ void __launch_bounds__(PC_WARPS * 32)
-route_permute_kernel(const float* __restrict__ z, const float* __restrict__ bias, int32_t* __restrict__ idx, float* __restrict__ gate,
+route_permute_kernel(const float* z, const float* bias, int32_t* __restrict__ idx, float* __restrict__ gate,
                      int32_t* __restrict__ counts, int32_t* __restrict__ offsets, int32_t* __restrict__ perm_row,
                      int32_t* __restrict__ row_src, int T, int E, int k, int score_fn, int bias_mode, int per_cta,
-                     int32_t* __restrict__ tile_table, const uint4* __restrict__ x, uint4* __restrict__ Xp, int vec_per_row) {
+                     int32_t* __restrict__ tile_table, const uint4* x, uint4* __restrict__ Xp, int vec_per_row) {
     extern __shared__ int32_t perm_smem[];
     const PermSmem sm(perm_smem, E);
     int32_t* rows = sm.wsum + 32;                      // [per_cta][k] rows of this CTA's assignments
@@ -60,7 +60,7 @@ route_permute_kernel(const float* __restrict__ z, const float* __restrict__ bias
         uint4 v[V];
 #pragma unroll
         for (int q = 0; q < V; ++q)
-            if (c + 32 * q < vec_per_row) v[q] = __ldg(s + 32 * q);
+            if (c + 32 * q < vec_per_row) v[q] = s[32 * q];
         for (int j = 0; j < k; ++j) {
             uint4* o = Xp + (size_t)rows[t * k + j] * vec_per_row + c;
 #pragma unroll

@@ -59,7 +59,7 @@ __device__ __forceinline__ void lds_b128(uint32_t addr, uint32_t (&v)[4]) {
 
 template <int RT, int RE, int LT, int CW, bool TWO>
 __global__ void __launch_bounds__(ScoreShape<RT, RE, LT, CW, TWO>::THREADS, TWO ? 2 : 0)
-route_score_kernel(const bf16* __restrict__ x, const float* __restrict__ W_r, float* __restrict__ z, int T, int d, int E,
+route_score_kernel(const bf16* x, const float* W_r, float* __restrict__ z, int T, int d, int E,
                    int32_t* __restrict__ status) {
     using Sh = ScoreShape<RT, RE, LT, CW, TWO>;
     constexpr bool PAIRS = Sh::PAIRS;

@@ -33,10 +33,7 @@ def test_another_ctas_shared_memory_is_used_only_after_a_cluster_barrier(path):
             assert not uses or "cluster_sync_all()" in body[:min(uses)], body[:160]
 
 
-LAUNCHED_EARLY = [CSRC / "balance.cuh", CSRC / "distill.cuh"]
-
-
-@pytest.mark.parametrize("path", LAUNCHED_EARLY, ids=lambda p: p.name)
+@pytest.mark.parametrize("path", SOURCES, ids=lambda p: p.name)
 def test_nothing_is_read_through_the_read_only_path(path):
     """A kernel that programmatic launches bring up early lives while the one before it still writes, and a read-only load (__ldg, or a
     kernel's `const ... * __restrict__` parameter, which the compiler may turn into one) is defined only for memory that nobody writes
