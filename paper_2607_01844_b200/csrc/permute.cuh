@@ -21,10 +21,12 @@ __global__ void __launch_bounds__(PERM_WARPS * 32) perm_hist_kernel(const int32_
     if (a0 >= M) return;
     for (int e = lane; e < E; e += 32) cnt[e] = 0;
     __syncwarp();
+    int ev[PERM_SEG / 32];                                 // all in flight before the first is counted
+#pragma unroll
+    for (int it = 0; it < PERM_SEG / 32; ++it) ev[it] = a0 + it * 32 + lane < M ? idx[a0 + it * 32 + lane] : -1;
+#pragma unroll
     for (int it = 0; it < PERM_SEG / 32; ++it) {
-        const int a = a0 + it * 32 + lane;
-        int e = (a < M) ? idx[a] : -1;
-        if (e < 0 || e >= E) e = -1;
+        const int e = ev[it] < E ? max(ev[it], -1) : -1;
         const uint32_t same = __match_any_sync(0xffffffffu, e);
         if (e >= 0 && lane == __ffs(same) - 1) cnt[e] += __popc(same);
         __syncwarp();
