@@ -77,11 +77,22 @@ __device__ __forceinline__ void bal_scores(const BalShape& s, float (&z)[4 * NV]
 #pragma unroll
         for (int i = 0; i < 4 * NV; ++i) { z[i] = __expf(z[i] - m); sum += z[i]; }
     } else {
+        // The scores of a row that lies far below zero are taken relative to its largest: below -87 they, and below -88 the reciprocal of
+        // their sum, leave the range of fp32.  (Such a row: no lane of the group has a logit of -16 or more.)
+        float m = z[0], shift = 0.0f;
+#pragma unroll
+        for (int i = 1; i < 4 * NV; ++i) m = fmaxf(m, z[i]);
+        const uint32_t near = __ballot_sync(0xffffffffu, m >= -16.0f);
+        const bool far = (near & (0xffffffffu >> (32 - s.G)) << (threadIdx.x % 32 & ~(s.G - 1))) == 0;
+        if (__any_sync(0xffffffffu, far)) {
+            for (int o = s.G >> 1; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+            if (far && m > -INFINITY) shift = m;
+        }
 #pragma unroll
         for (int i = 0; i < 4 * NV; ++i) {
             const float e = __expf(-fabsf(z[i])), r = __fdividef(1.0f, 1.0f + e);
             oms[i] = z[i] >= 0.0f ? e * r : r;
-            z[i] = z[i] >= 0.0f ? r : (z[i] < 0.0f ? e * r : z[i]);      // (NaN stays)
+            z[i] = z[i] >= 0.0f ? r : (z[i] < 0.0f ? (shift == 0.0f ? e : __expf(z[i] - shift)) * r : z[i]);      // (NaN stays)
             sum += z[i];
         }
     }
