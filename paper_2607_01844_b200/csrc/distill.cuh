@@ -504,14 +504,18 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
             } else {
                 const bool mine = row < args.N;
                 float coef = 0.0f, lse2 = 0.0f;
-                bool inside = true;
+                bool inside = true, padding = false;
                 float scale[4] = {};
-                (void)scale;
+                (void)scale; (void)padding;
                 if constexpr (KIND == VD_R) {
                     if (mine) coef = args.row_scale[row];
 #pragma unroll
                     for (int g = 0; g < 4; ++g) scale[g] = args.col_scale[col0 / 32 + g];
-                    if (args.add_to && args.seq_off) inside = row >= args.seq_off[0] && row < args.seq_off[args.n_seq];
+                    if (args.seq_off) {
+                        const int begin = args.seq_off[0], end = args.seq_off[args.n_seq], r0 = row - (quarter * 32 + lane);
+                        inside = row >= begin && row < end;
+                        padding = r0 < begin || min(r0 + 128, args.N) > end;       // among the CTA's 128 rows
+                    }
                 }
                 VdEntries en;
                 (void)en;
@@ -564,20 +568,34 @@ vd_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ 
 #pragma unroll
                         for (int i = 0; i < 32; ++i) y[g][i] *= scale[g];
                     }
-                    if (args.add_to && mine) {
+                    if (padding && !inside)               // (0 times a router weight that is not finite)
+#pragma unroll
+                        for (int g = 0; g < 4; ++g)
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) y[g][i] = 0.0f;
+                    if (args.add_to && mine && inside) {
 #pragma unroll
                         for (int j = 0; j < 16; ++j) {
                             if (col0 + 8 * j >= args.cols) continue;
                             float* v = &y[j / 4][(j % 4) * 8];
                             const uint4 o = *reinterpret_cast<const uint4*>(args.add_to + (size_t)row * args.cols + col0 + 8 * j);
-                            if (inside) {
-                                v[0] += bf16_lo(o.x); v[1] += bf16_hi(o.x); v[2] += bf16_lo(o.y); v[3] += bf16_hi(o.y);
-                                v[4] += bf16_lo(o.z); v[5] += bf16_hi(o.z); v[6] += bf16_lo(o.w); v[7] += bf16_hi(o.w);
-                            } else {                      // (the rounding below gives back the same bits)
-                                v[0] = bf16_lo(o.x); v[1] = bf16_hi(o.x); v[2] = bf16_lo(o.y); v[3] = bf16_hi(o.y);
-                                v[4] = bf16_lo(o.z); v[5] = bf16_hi(o.z); v[6] = bf16_lo(o.w); v[7] = bf16_hi(o.w);
-                            }
+                            v[0] += bf16_lo(o.x); v[1] += bf16_hi(o.x); v[2] += bf16_lo(o.y); v[3] += bf16_hi(o.y);
+                            v[4] += bf16_lo(o.z); v[5] += bf16_hi(o.z); v[6] += bf16_lo(o.w); v[7] += bf16_hi(o.w);
                         }
+                    }
+                    // Where padding is to stay as it is, a box with some of it is written by rows: a copy of the box would read and
+                    // write it again, and a NaN in it would not keep its bits.
+                    if (args.add_to && padding) {
+                        if (mine && inside)
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) {
+                                if (col0 + 8 * j >= args.cols) continue;
+                                const float* v = &y[j / 4][(j % 4) * 8];
+                                *reinterpret_cast<uint4*>(args.add_to + (size_t)row * args.cols + col0 + 8 * j) =
+                                    make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7]));
+                            }
+                        if (issuer) tma_store_commit();       // (an empty group: the box sets are told apart by counting groups)
+                        continue;
                     }
                 }
                 if constexpr (KIND == VD_P && !PAIR) {    // the teacher's entries, and two pieces: 64 rows of each in a box, or 128 in turn

@@ -53,3 +53,39 @@ def test_sigmoid_scores_of_a_row_of_the_lowest_logits():
     _, prob, loss = c.forward()
     assert float((prob[0] * 24 - 1).abs().max()) <= 1.3e-5 and abs(float(loss[0]) - 1) <= 2.6e-5
     assert float(prob[1].abs().max()) == 0.0 and float(loss[1]) == 0.0
+
+
+PADDED = [(300, 200, 20, [11, 60, 60, 61, 290]), (700, 72, 40, [130, 140]), (513, 264, 130, [0, 512]), (600, 64, 8, [300, 300]),
+          (2400, 1032, 64, [700, 1100, 1700])]       # whole tiles of padding among the others
+
+
+@pytest.mark.parametrize("T,d,E,off", PADDED, ids=lambda v: str(v) if isinstance(v, int) else "")
+def test_accumulating_leaves_rows_of_padding_to_the_bit(T, d, E, off):
+    """dX of padding tokens may hold anything, NaN of any pattern among it."""
+    c = Case(T, d, E, 3, SIGMOID, PRE, off, seed=T)
+    counts = c.forward()[0]
+    out = c.outputs(0.5)
+    bits = torch.randint(-32768, 32768, (T, d), device="cuda", dtype=torch.int32).to(torch.int16)
+    bits[:, ::5] = 0x7F81                                 # a signalling NaN
+    bits[:, 1::5] = -1                                    # a negative one with every bit set
+    raw = out["dX"].view(torch.int16)
+    raw[c.pad] = bits[c.pad]
+    c.backward(counts, out, True)
+    assert torch.equal(raw[c.pad], bits[c.pad])
+    raw[c.pad] = c.outputs(0.5)["dX"].view(torch.int16)[c.pad]
+    check_backward(c, out, 0.5, True)
+
+
+@pytest.mark.parametrize("T,d,E,off", PADDED, ids=lambda v: str(v) if isinstance(v, int) else "")
+@pytest.mark.parametrize("value", [float("inf"), float("nan")], ids=["inf", "nan"])
+def test_router_weights_that_are_not_finite_leave_padding_alone(T, d, E, off, value):
+    c = Case(T, d, E, 3, SIGMOID, PRE, off, seed=T)
+    c.W_r[5, 1] = value
+    counts = c.forward()[0]
+    out = c.backward(counts, c.outputs())
+    assert float(out["dX"][c.pad].abs().max()) == 0.0
+    kept = c.outputs(0.5)
+    c.backward(counts, kept, True)
+    assert bool((kept["dX"][c.pad] == 0.5).all())
+    inside = out["dX"][~c.pad].float()
+    assert not torch.isfinite(inside[:, 5]).any() or inside.numel() == 0
