@@ -274,7 +274,9 @@ mop_status mop_moe_balance_loss_fwd(mop_ctx* ctx, int32_t n_seq, const float* lo
  *   dW_r = x^T dz,   dX = dz W_r^T,   dbias = column sums of dz (MOP_BIAS_PRE_LOGIT; zero in the other modes)
  * and dz = 0 for padding tokens.  accumulate = 0 overwrites dW_r, dbias and dX (rows of padding tokens get zeros); 1 adds to them
  * (rows of padding tokens stay as they are), as is wanted behind mop_moe_route_bwd, which writes dW_r and adds to the same dX.
- * dlogits is always overwritten.  Any of the four outputs may be NULL, not all.  dW_r has fp32 accuracy; dX is rounded to bf16 once.
+ * dlogits is always overwritten.  Any of the four outputs may be NULL, not all.  dW_r has fp32 accuracy.  dX is rounded to bf16 once, from
+ * products of operands of 11 bits: a token's row of dz is scaled by one power of two and so are the rows 32 i to 32 i + 31 of W_r, and
+ * what lies 2^-28 or further below the largest of such a group keeps fewer bits (MOP_GEMM_SCALAR: fp32 throughout).
  * counts [n_seq,E] i32 from the forward (or their totals over several devices: dz is linear in them); dloss [n_seq] f32;
  * x [T,d] bf16 (needed for dW_r; rows of padding tokens are not read into it, whatever they hold); W_r [d,E] f32 (needed for dX);
  * dlogits_opt [T,E] f32, dW_r_opt [d,E] f32, dbias_opt [E] f32, dX_opt [T,d] bf16 out; workspace:

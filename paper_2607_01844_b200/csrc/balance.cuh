@@ -347,7 +347,10 @@ __device__ __forceinline__ void bal_convert_w(const BalBwdArgs& a, int block, in
         float amax = 0.0f, up, down;
         for (int r = r0 + warp; r < min(r0 + 32, a.d); r += warps)
 #pragma unroll 4
-            for (int e = lane; e < E; e += 32) amax = fmaxf(amax, fabsf(a.W_r[(size_t)r * E + e]));
+            for (int e = lane; e < E; e += 32) {
+                const float w = fabsf(a.W_r[(size_t)r * E + e]);
+                amax = fmaxf(amax, w < INFINITY ? w : 0.0f);       // (an infinity stays one, the rows beside it keep their digits)
+            }
         for (int o = 16; o > 0; o >>= 1) amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
         __syncthreads();
         if (lane == 0) amax_of[warp] = amax;

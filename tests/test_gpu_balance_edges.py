@@ -89,3 +89,16 @@ def test_router_weights_that_are_not_finite_leave_padding_alone(T, d, E, off, va
     assert bool((kept["dX"][c.pad] == 0.5).all())
     inside = out["dX"][~c.pad].float()
     assert not torch.isfinite(inside[:, 5]).any() or inside.numel() == 0
+
+
+@pytest.mark.parametrize("value", [float("inf"), -float("inf"), float("nan")], ids=["inf", "minus-inf", "nan"])
+def test_a_router_weight_that_is_not_finite_shows_in_its_column_of_dX_only(value):
+    """A column of dX is one row of W_r; the rows that share its scale keep their digits."""
+    c = Case(200, 136, 24, 4, SOFTMAX, NONE, [0, 90, 200], seed=8)
+    counts = c.forward()[0]
+    c.W_r[37, 3] = 0.0
+    want = c.backward(counts, c.outputs())["dX"]
+    c.W_r[37, 3] = value
+    got = c.backward(counts, c.outputs())["dX"]
+    other = torch.arange(136, device="cuda") != 37
+    assert torch.equal(got[:, other], want[:, other]) and not torch.isfinite(got[:, 37]).any()
