@@ -1683,6 +1683,14 @@ mop_status vocab_plan(int device, TcPlan** out) {
     *out = p;
     return MOP_OK;
 }
+// What a call without tokens owes mop_vocab_poll: a clean status word, whatever the workspace held (a caller may pass none).
+mop_status vocab_clear_status(int device, void* workspace, void* stream) {
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || device < 0 || device >= kMaxDevices) return MOP_OK;
+    DeviceGuard guard(device);
+    if (!guard.ok) return MOP_ERR_CUDA;
+    CUDA_OK(cudaMemsetAsync(workspace, 0, 4, static_cast<cudaStream_t>(stream)));
+    return MOP_OK;
+}
 }  // namespace
 
 size_t mop_vocab_workspace_bytes(int32_t N, int32_t H, int32_t V) {
@@ -1695,7 +1703,7 @@ mop_status mop_vocab_loss_fwd(int device, int32_t N, int32_t H, int32_t V, const
     if (N < 0 || H < 1 || V < 1) return MOP_ERR_INVALID_ARG;
     if (H % 64 || V % 64) return MOP_ERR_UNSUPPORTED;
     if ((long long)N * 2 >= (1ll << 31) || (long long)H * V >= (1ll << 40)) return MOP_ERR_SHAPE;
-    if (N == 0) return MOP_OK;
+    if (N == 0) return vocab_clear_status(device, workspace, stream);
     if (!X || !W_voc || !targets || !loss || !workspace) return MOP_ERR_INVALID_ARG;
     if (!aligned16(X) || !aligned16(W_voc) || !aligned16(targets) || !aligned16(loss) ||
         (reinterpret_cast<uintptr_t>(workspace) & 255u) || (lse_opt && !aligned16(lse_opt)))
@@ -1803,7 +1811,7 @@ mop_status mop_vocab_loss_bwd(int device, int32_t N, int32_t H, int32_t V, const
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (N == 0) {   // no tokens: the weight gradient is zero
         CUDA_OK(cudaMemsetAsync(dW_voc, 0, (size_t)H * V * 4, st));
-        return MOP_OK;
+        return vocab_clear_status(device, workspace, stream);
     }
     TcPlan* p = nullptr;
     mop_status r = vocab_plan(device, &p);
@@ -1935,7 +1943,7 @@ mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, in
                                  float temperature, float* loss, float* student, float* lse, void* workspace, void* stream) {
     mop_status r = distill_check(device, N, H, V, K, temperature);
     if (r != MOP_OK) return r;
-    if (N == 0) return MOP_OK;
+    if (N == 0) return vocab_clear_status(device, workspace, stream);
     if (!X || !W_voc || !teacher_idx || !teacher_logits || !loss || !student || !lse || !workspace) return MOP_ERR_INVALID_ARG;
     if (!aligned16(X) || !aligned16(W_voc) || !aligned16(teacher_idx) || !aligned16(teacher_logits) || !aligned16(teacher_lse_opt) ||
         !aligned16(loss) || !aligned16(student) || !aligned16(lse) || (reinterpret_cast<uintptr_t>(workspace) & 255u))
@@ -1994,7 +2002,7 @@ mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, in
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (N == 0) {   // no tokens: the weight gradient is zero
         CUDA_OK(cudaMemsetAsync(dW_voc, 0, (size_t)H * V * 2, st));
-        return MOP_OK;
+        return vocab_clear_status(device, workspace, stream);
     }
     TcPlan* p = nullptr;
     if ((r = vocab_plan(device, &p)) != MOP_OK) return r;
