@@ -6,6 +6,7 @@ if the shared library is missing, importing this module's `lib()` raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 from pathlib import Path
 
@@ -117,6 +118,14 @@ def _stream(stream):
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _workspace(size, device, stream):
+    """Memory for a call on `stream`, from that stream's pool of the allocator: once freed it goes to calls behind this one, also where the
+    current stream is another one.  Who uses it on further streams records them."""
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(
+            stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)):
+        return torch.empty(max(256, size), dtype=torch.uint8, device=device)
 
 
 def _check(call, rc):
@@ -341,7 +350,7 @@ def mop_vocab_loss_fwd(device, X, W_voc, targets, loss, lse=None, workspace=None
     N, H = X.shape
     V = W_voc.shape[1]
     if workspace is None:
-        workspace = torch.empty(max(256, mop_vocab_workspace_bytes(N, H, V)), dtype=torch.uint8, device=X.device)
+        workspace = _workspace(mop_vocab_workspace_bytes(N, H, V), X.device, stream)
     _check("mop_vocab_loss_fwd",
            lib().mop_vocab_loss_fwd(device, N, H, V, _ptr(X), _ptr(W_voc), _ptr(targets), _ptr(loss), _ptr(lse),
                                     _ptr(workspace), _stream(stream)))
@@ -366,7 +375,7 @@ def mop_vocab_loss_bwd(device, X, W_voc, targets, lse, dloss, dX, dW_voc, worksp
     N, H = X.shape
     V = W_voc.shape[1]
     if workspace is None:
-        workspace = torch.empty(max(256, mop_vocab_bwd_workspace_bytes(N, H, V)), dtype=torch.uint8, device=X.device)
+        workspace = _workspace(mop_vocab_bwd_workspace_bytes(N, H, V), X.device, stream)
     _check("mop_vocab_loss_bwd",
            lib().mop_vocab_loss_bwd(device, N, H, V, _ptr(X), _ptr(W_voc), _ptr(targets), _ptr(lse), _ptr(dloss),
                                     _ptr(dX), _ptr(dW_voc), _ptr(workspace), _stream(stream)))
@@ -382,7 +391,7 @@ def mop_vocab_distill_fwd(device, X, W_voc, teacher_idx, teacher_logits, tempera
     """loss[n] = KL divergence of the student from the teacher over the teacher's entries; student = logits at those entries."""
     (N, H), V, K = X.shape, W_voc.shape[1], teacher_idx.shape[1]
     if workspace is None:
-        workspace = torch.empty(max(256, mop_vocab_distill_workspace_bytes(N, H, V, K)), dtype=torch.uint8, device=X.device)
+        workspace = _workspace(mop_vocab_distill_workspace_bytes(N, H, V, K), X.device, stream)
     _check("mop_vocab_distill_fwd",
            lib().mop_vocab_distill_fwd(device, N, H, V, K, _ptr(X), _ptr(W_voc), _ptr(teacher_idx), _ptr(teacher_logits),
                                        _ptr(teacher_lse), temperature, _ptr(loss), _ptr(student), _ptr(lse), _ptr(workspace),
@@ -399,7 +408,7 @@ def mop_vocab_distill_bwd(device, X, W_voc, teacher_idx, teacher_logits, tempera
     """dX, dW_voc of sum_n dloss[n] loss[n]; student and lse are the forward's."""
     (N, H), V, K = X.shape, W_voc.shape[1], teacher_idx.shape[1]
     if workspace is None:
-        workspace = torch.empty(max(256, mop_vocab_distill_bwd_workspace_bytes(N, H, V, K)), dtype=torch.uint8, device=X.device)
+        workspace = _workspace(mop_vocab_distill_bwd_workspace_bytes(N, H, V, K), X.device, stream)
     _check("mop_vocab_distill_bwd",
            lib().mop_vocab_distill_bwd(device, N, H, V, K, _ptr(X), _ptr(W_voc), _ptr(teacher_idx), _ptr(teacher_logits),
                                        _ptr(teacher_lse), temperature, _ptr(student), _ptr(lse), _ptr(dloss), _ptr(dX),

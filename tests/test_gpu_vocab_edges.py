@@ -26,3 +26,37 @@ def test_a_poll_after_a_call_without_tokens_finds_nothing():
         call()
         binding.mop_vocab_poll(0, ws)
     assert float(dW.abs().max()) == 0.0 and float(dW32.abs().max()) == 0.0
+
+
+def vocab_calls(stream):
+    """The four calls with a workspace of their own, on `stream`; each returns it."""
+    N, H, V, K = 300, 64, 1024, 5
+    g = torch.Generator(device="cuda").manual_seed(1)
+    X = torch.randn((N, H), generator=g, device="cuda").to(torch.bfloat16)
+    W = torch.randn((H, V), generator=g, device="cuda").to(torch.bfloat16)
+    ids = torch.randint(0, V, (N, K), generator=g, device="cuda", dtype=torch.int32)
+    t, f = torch.randn((N, K), generator=g, device="cuda"), torch.zeros((N,), device="cuda")
+    loss, lse, student = torch.zeros_like(f), torch.zeros_like(f), torch.zeros_like(t)
+    targets, dX, dW, dW32 = ids[:, 0].contiguous(), torch.empty_like(X), torch.empty_like(W), torch.empty((H, V), device="cuda")
+    yield lambda: binding.mop_vocab_distill_fwd(0, X, W, ids, t, 1.0, loss, student, lse, None, None, stream)
+    yield lambda: binding.mop_vocab_distill_bwd(0, X, W, ids, t, 1.0, student, lse, f, dX, dW, None, None, stream)
+    yield lambda: binding.mop_vocab_loss_fwd(0, X, W, targets, loss, lse, None, stream)
+    yield lambda: binding.mop_vocab_loss_bwd(0, X, W, targets, lse, f, dX, dW32, None, stream)
+
+
+@pytest.mark.parametrize("raw", [False, True], ids=["stream", "handle"])
+def test_a_default_workspace_belongs_to_the_stream_of_the_call(raw):
+    """Dropped while the call is in flight, it is not handed to an allocation of the current stream, but to the call's next one."""
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    for call in vocab_calls(side.cuda_stream if raw else side):
+        torch.cuda.synchronize()
+        torch.cuda.empty_cache()
+        workspace = call()
+        at, size = workspace.data_ptr(), workspace.numel()
+        del workspace
+        here = [torch.empty((size,), dtype=torch.uint8, device="cuda") for _ in range(4)]
+        assert at not in [t.data_ptr() for t in here]
+        with torch.cuda.stream(side):
+            assert torch.empty((size,), dtype=torch.uint8, device="cuda").data_ptr() == at
+    side.synchronize()
