@@ -112,11 +112,17 @@ def _ptr(t):
     return t.data_ptr()
 
 
-def _stream(stream):
+def _stream(stream, device=None):
     if stream is None:
-        # the current stream's handle without building a Stream object around it (3 us of a small layer's 50), where torch has it
+        # the current stream's handle without building a Stream object around it (3 us of a small layer's 50), where torch has it; that of
+        # the device the call runs on, which need not be the current one
         raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-        return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
+        if raw is None:
+            return (torch.cuda.current_stream() if device is None else torch.cuda.current_stream(device)).cuda_stream
+        try:
+            return raw(torch.cuda.current_device() if device is None else device)
+        except RuntimeError:             # no such device: the library says so
+            return raw(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -141,6 +147,7 @@ class Context:
         self.shape = MopShape(T, d, E, k, f, score_fn, bias_mode, int(with_backward), int(dw_accumulate), gemm_path,
                               int(host_io), route_path)
         self.handle = _P()
+        self.device = device
         _check("mop_create", lib().mop_create(ctypes.byref(self.handle), ctypes.byref(self.shape), device))
 
     def close(self):
@@ -164,31 +171,31 @@ class Context:
 
 
 def mop_poll(ctx, stream=None):
-    _check("mop_poll", lib().mop_poll(ctx.handle, _stream(stream)))
+    _check("mop_poll", lib().mop_poll(ctx.handle, _stream(stream, ctx.device)))
 
 
 def mop_selftest_wait_timeout(ctx, limit_cycles=20_000_000, stream=None):
-    _check("mop_selftest_wait_timeout", lib().mop_selftest_wait_timeout(ctx.handle, limit_cycles, _stream(stream)))
+    _check("mop_selftest_wait_timeout", lib().mop_selftest_wait_timeout(ctx.handle, limit_cycles, _stream(stream, ctx.device)))
 
 
 def mop_debug_guard_arm(ctx, stream=None):
-    _check("mop_debug_guard_arm", lib().mop_debug_guard_arm(ctx.handle, _stream(stream)))
+    _check("mop_debug_guard_arm", lib().mop_debug_guard_arm(ctx.handle, _stream(stream, ctx.device)))
 
 
 def mop_debug_guard_poke(ctx, band, byte, stream=None):
-    _check("mop_debug_guard_poke", lib().mop_debug_guard_poke(ctx.handle, band, byte, _stream(stream)))
+    _check("mop_debug_guard_poke", lib().mop_debug_guard_poke(ctx.handle, band, byte, _stream(stream, ctx.device)))
 
 
 def mop_debug_guard_check(ctx, stream=None):
     """Bytes of the workspace's guard bands that were overwritten since they were armed."""
     bad = ctypes.c_int64(-1)
-    _check("mop_debug_guard_check", lib().mop_debug_guard_check(ctx.handle, ctypes.byref(bad), _stream(stream)))
+    _check("mop_debug_guard_check", lib().mop_debug_guard_check(ctx.handle, ctypes.byref(bad), _stream(stream, ctx.device)))
     return bad.value
 
 
 def mop_moe_route(ctx, x, W_r, bias, topk_idx, topk_gate, logits=None, stream=None):
     _check("mop_moe_route", lib().mop_moe_route(ctx.handle, _ptr(x), _ptr(W_r), _ptr(bias), _ptr(topk_idx),
-                                                _ptr(topk_gate), _ptr(logits), _stream(stream)))
+                                                _ptr(topk_gate), _ptr(logits), _stream(stream, ctx.device)))
 
 
 def mop_route_stats(ctx, stream=None):
@@ -196,13 +203,13 @@ def mop_route_stats(ctx, stream=None):
     tensor-core scoring path since the last call."""
     a, b, c = ctypes.c_int64(0), ctypes.c_int64(0), ctypes.c_int64(0)
     _check("mop_route_stats", lib().mop_route_stats(ctx.handle, ctypes.byref(a), ctypes.byref(b), ctypes.byref(c),
-                                                    _stream(stream)))
+                                                    _stream(stream, ctx.device)))
     return a.value, b.value, c.value
 
 
 def mop_moe_permute(ctx, x, topk_idx, counts, offsets, perm_row, row_src, Xp, stream=None):
     _check("mop_moe_permute", lib().mop_moe_permute(ctx.handle, _ptr(x), _ptr(topk_idx), _ptr(counts), _ptr(offsets),
-                                                    _ptr(perm_row), _ptr(row_src), _ptr(Xp), _stream(stream)))
+                                                    _ptr(perm_row), _ptr(row_src), _ptr(Xp), _stream(stream, ctx.device)))
 
 
 def mop_moe_expert_ffn_fwd(ctx, Xp, offsets, row_src, topk_gate, W_gate, W_up, W_down, G_save, U_save, H, Yp,
@@ -210,18 +217,18 @@ def mop_moe_expert_ffn_fwd(ctx, Xp, offsets, row_src, topk_gate, W_gate, W_up, W
     _check("mop_moe_expert_ffn_fwd",
            lib().mop_moe_expert_ffn_fwd(ctx.handle, _ptr(Xp), _ptr(offsets), _ptr(row_src), _ptr(topk_gate),
                                         _ptr(W_gate), _ptr(W_up), _ptr(W_down), _ptr(G_save), _ptr(U_save), _ptr(H),
-                                        _ptr(Yp), _stream(stream)))
+                                        _ptr(Yp), _stream(stream, ctx.device)))
 
 
 def mop_moe_expert_ffn_fwd_gather(ctx, x, offsets, row_src, topk_gate, W_gate, W_up, W_down, H, Yp, stream=None):
     _check("mop_moe_expert_ffn_fwd_gather",
            lib().mop_moe_expert_ffn_fwd_gather(ctx.handle, _ptr(x), _ptr(offsets), _ptr(row_src), _ptr(topk_gate),
                                                _ptr(W_gate), _ptr(W_up), _ptr(W_down), _ptr(H), _ptr(Yp),
-                                               _stream(stream)))
+                                               _stream(stream, ctx.device)))
 
 
 def mop_moe_combine(ctx, Yp, perm_row, Y, stream=None):
-    _check("mop_moe_combine", lib().mop_moe_combine(ctx.handle, _ptr(Yp), _ptr(perm_row), _ptr(Y), _stream(stream)))
+    _check("mop_moe_combine", lib().mop_moe_combine(ctx.handle, _ptr(Yp), _ptr(perm_row), _ptr(Y), _stream(stream, ctx.device)))
 
 
 def mop_moe_layer_fwd(ctx, x, W_r, bias, W_gate, W_up, W_down, topk_idx, topk_gate, counts, offsets, perm_row, row_src, Xp,
@@ -231,7 +238,7 @@ def mop_moe_layer_fwd(ctx, x, W_r, bias, W_gate, W_up, W_down, topk_idx, topk_ga
            lib().mop_moe_layer_fwd(ctx.handle, _ptr(x), _ptr(W_r), _ptr(bias), _ptr(W_gate), _ptr(W_up), _ptr(W_down),
                                    _ptr(topk_idx), _ptr(topk_gate), _ptr(counts), _ptr(offsets), _ptr(perm_row),
                                    _ptr(row_src), _ptr(Xp), _ptr(G_save), _ptr(U_save), _ptr(H), _ptr(Yp), _ptr(Y),
-                                   _stream(stream)))
+                                   _stream(stream, ctx.device)))
 
 
 def mop_moe_expert_ffn_bwd(ctx, dY, Xp, G_save, U_save, H, offsets, perm_row, row_src, topk_gate, W_gate, W_up,
@@ -240,7 +247,7 @@ def mop_moe_expert_ffn_bwd(ctx, dY, Xp, G_save, U_save, H, offsets, perm_row, ro
            lib().mop_moe_expert_ffn_bwd(ctx.handle, _ptr(dY), _ptr(Xp), _ptr(G_save), _ptr(U_save), _ptr(H),
                                         _ptr(offsets), _ptr(perm_row), _ptr(row_src), _ptr(topk_gate), _ptr(W_gate),
                                         _ptr(W_up), _ptr(W_down), _ptr(dX), _ptr(dW_gate), _ptr(dW_up), _ptr(dW_down),
-                                        _ptr(dgate), _stream(stream)))
+                                        _ptr(dgate), _stream(stream, ctx.device)))
 
 
 def mop_moe_route_bwd(ctx, logits, bias, topk_idx, topk_gate, dgate, Xp, offsets, perm_row, W_r, dW_r, dbias, dX,
@@ -248,7 +255,7 @@ def mop_moe_route_bwd(ctx, logits, bias, topk_idx, topk_gate, dgate, Xp, offsets
     _check("mop_moe_route_bwd",
            lib().mop_moe_route_bwd(ctx.handle, _ptr(logits), _ptr(bias), _ptr(topk_idx), _ptr(topk_gate), _ptr(dgate),
                                    _ptr(Xp), _ptr(offsets), _ptr(perm_row), _ptr(W_r), _ptr(dW_r), _ptr(dbias),
-                                   _ptr(dX), _stream(stream)))
+                                   _ptr(dX), _stream(stream, ctx.device)))
 
 
 def mop_moe_balance_workspace_bytes(ctx, n_seq, with_backward=False):
@@ -259,7 +266,7 @@ def mop_moe_balance_loss_fwd(ctx, logits, bias, topk_idx, seq_offsets, counts, p
     """Per sequence of a packed batch: expert counts, mean scores and the load-balance loss."""
     _check("mop_moe_balance_loss_fwd",
            lib().mop_moe_balance_loss_fwd(ctx.handle, loss.shape[0], _ptr(logits), _ptr(bias), _ptr(topk_idx), _ptr(seq_offsets),
-                                          _ptr(counts), _ptr(prob), _ptr(loss), _ptr(workspace), _stream(stream)))
+                                          _ptr(counts), _ptr(prob), _ptr(loss), _ptr(workspace), _stream(stream, ctx.device)))
 
 
 def mop_moe_balance_loss_bwd(ctx, logits, bias, seq_offsets, counts, dloss, x, W_r, dlogits, dW_r, dbias, dX, accumulate, workspace,
@@ -268,7 +275,7 @@ def mop_moe_balance_loss_bwd(ctx, logits, bias, seq_offsets, counts, dloss, x, W
     _check("mop_moe_balance_loss_bwd",
            lib().mop_moe_balance_loss_bwd(ctx.handle, dloss.shape[0], _ptr(logits), _ptr(bias), _ptr(seq_offsets), _ptr(counts),
                                           _ptr(dloss), _ptr(x), _ptr(W_r), int(accumulate), _ptr(dlogits), _ptr(dW_r), _ptr(dbias),
-                                          _ptr(dX), _ptr(workspace), _stream(stream)))
+                                          _ptr(dX), _ptr(workspace), _stream(stream, ctx.device)))
 
 
 def mop_moe_chunked_workspace_bytes(ctx, n_chunks, with_backward=False):
@@ -281,7 +288,7 @@ def mop_moe_layer_fwd_chunked(ctx, n_chunks, x, W_r, bias, W_gate, W_up, W_down,
     _check("mop_moe_layer_fwd_chunked",
            lib().mop_moe_layer_fwd_chunked(ctx.handle, n_chunks, _ptr(x), _ptr(W_r), _ptr(bias), _ptr(W_gate), _ptr(W_up),
                                            _ptr(W_down), _ptr(topk_idx), _ptr(topk_gate), _ptr(counts), _ptr(offsets),
-                                           _ptr(perm_row), _ptr(row_src), _ptr(Y), _ptr(workspace), _stream(stream)))
+                                           _ptr(perm_row), _ptr(row_src), _ptr(Y), _ptr(workspace), _stream(stream, ctx.device)))
 
 
 def mop_moe_layer_bwd_chunked(ctx, n_chunks, x, dY, topk_gate, offsets, perm_row, row_src, W_gate, W_up, W_down, dX,
@@ -291,7 +298,7 @@ def mop_moe_layer_bwd_chunked(ctx, n_chunks, x, dY, topk_gate, offsets, perm_row
            lib().mop_moe_layer_bwd_chunked(ctx.handle, n_chunks, _ptr(x), _ptr(dY), _ptr(topk_gate), _ptr(offsets),
                                            _ptr(perm_row), _ptr(row_src), _ptr(W_gate), _ptr(W_up), _ptr(W_down),
                                            _ptr(dX), _ptr(dW_gate), _ptr(dW_up), _ptr(dW_down), _ptr(dgate),
-                                           _ptr(workspace), _stream(stream)))
+                                           _ptr(workspace), _stream(stream, ctx.device)))
 
 
 def mop_moe_forward_host(ctx, x_host, W_r, bias, W_gate, W_up, W_down, Y_host, idx_host=None, gate_host=None,
@@ -299,7 +306,7 @@ def mop_moe_forward_host(ctx, x_host, W_r, bias, W_gate, W_up, W_down, Y_host, i
     """x_host / Y_host / idx_host / gate_host are HOST tensors (pinned for full copy speed)."""
     _check("mop_moe_forward_host",
            lib().mop_moe_forward_host(ctx.handle, _ptr(x_host), _ptr(W_r), _ptr(bias), _ptr(W_gate), _ptr(W_up),
-                                      _ptr(W_down), _ptr(Y_host), _ptr(idx_host), _ptr(gate_host), _stream(stream)))
+                                      _ptr(W_down), _ptr(Y_host), _ptr(idx_host), _ptr(gate_host), _stream(stream, ctx.device)))
 
 
 def mop_moe_train_step_host(ctx, x_host, dY_host, W_r, bias, W_gate, W_up, W_down, Y_host, dX_host, dgate_host,
@@ -308,7 +315,7 @@ def mop_moe_train_step_host(ctx, x_host, dY_host, W_r, bias, W_gate, W_up, W_dow
     _check("mop_moe_train_step_host",
            lib().mop_moe_train_step_host(ctx.handle, _ptr(x_host), _ptr(dY_host), _ptr(W_r), _ptr(bias), _ptr(W_gate),
                                          _ptr(W_up), _ptr(W_down), _ptr(Y_host), _ptr(dX_host), _ptr(dgate_host),
-                                         _ptr(dW_gate), _ptr(dW_up), _ptr(dW_down), _stream(stream)))
+                                         _ptr(dW_gate), _ptr(dW_up), _ptr(dW_down), _stream(stream, ctx.device)))
 
 
 def mop_moe_forward_host_async(ctx, x_host, W_r, bias, W_gate, W_up, W_down, Y_host, idx_host=None, gate_host=None,
@@ -317,7 +324,7 @@ def mop_moe_forward_host_async(ctx, x_host, W_r, bias, W_gate, W_up, W_down, Y_h
     _check("mop_moe_forward_host_async",
            lib().mop_moe_forward_host_async(ctx.handle, _ptr(x_host), _ptr(W_r), _ptr(bias), _ptr(W_gate),
                                             _ptr(W_up), _ptr(W_down), _ptr(Y_host), _ptr(idx_host), _ptr(gate_host),
-                                            _stream(stream)))
+                                            _stream(stream, ctx.device)))
 
 
 def mop_moe_train_step_host_async(ctx, x_host, dY_host, W_r, bias, W_gate, W_up, W_down, Y_host, dX_host, dgate_host,
@@ -327,18 +334,18 @@ def mop_moe_train_step_host_async(ctx, x_host, dY_host, W_r, bias, W_gate, W_up,
            lib().mop_moe_train_step_host_async(ctx.handle, _ptr(x_host), _ptr(dY_host), _ptr(W_r), _ptr(bias),
                                                _ptr(W_gate), _ptr(W_up), _ptr(W_down), _ptr(Y_host), _ptr(dX_host),
                                                _ptr(dgate_host), _ptr(dW_gate), _ptr(dW_up), _ptr(dW_down),
-                                               _stream(stream)))
+                                               _stream(stream, ctx.device)))
 
 
 def mop_host_drain(ctx, stream=None):
-    _check("mop_host_drain", lib().mop_host_drain(ctx.handle, _stream(stream)))
+    _check("mop_host_drain", lib().mop_host_drain(ctx.handle, _stream(stream, ctx.device)))
 
 
 def mop_moe_permute_static(device, T, d, E, k, x, topk_idx, counts, offsets, perm_row, row_src, Xp, stream=None):
     """Permutation for callers that may not allocate: no context, scratch compiled into the library."""
     _check("mop_moe_permute_static",
            lib().mop_moe_permute_static(device, T, d, E, k, _ptr(x), _ptr(topk_idx), _ptr(counts), _ptr(offsets),
-                                        _ptr(perm_row), _ptr(row_src), _ptr(Xp), _stream(stream)))
+                                        _ptr(perm_row), _ptr(row_src), _ptr(Xp), _stream(stream, device)))
 
 
 def mop_vocab_workspace_bytes(N, H, V):
@@ -353,17 +360,17 @@ def mop_vocab_loss_fwd(device, X, W_voc, targets, loss, lse=None, workspace=None
         workspace = _workspace(mop_vocab_workspace_bytes(N, H, V), X.device, stream)
     _check("mop_vocab_loss_fwd",
            lib().mop_vocab_loss_fwd(device, N, H, V, _ptr(X), _ptr(W_voc), _ptr(targets), _ptr(loss), _ptr(lse),
-                                    _ptr(workspace), _stream(stream)))
+                                    _ptr(workspace), _stream(stream, device)))
     return workspace
 
 
 def mop_vocab_poll(device, workspace, stream=None):
-    _check("mop_vocab_poll", lib().mop_vocab_poll(device, _ptr(workspace), _stream(stream)))
+    _check("mop_vocab_poll", lib().mop_vocab_poll(device, _ptr(workspace), _stream(stream, device)))
 
 
 def mop_vocab_selftest_wait_timeout(device, workspace, limit_cycles=20_000_000, stream=None):
     _check("mop_vocab_selftest_wait_timeout",
-           lib().mop_vocab_selftest_wait_timeout(device, _ptr(workspace), limit_cycles, _stream(stream)))
+           lib().mop_vocab_selftest_wait_timeout(device, _ptr(workspace), limit_cycles, _stream(stream, device)))
 
 
 def mop_vocab_bwd_workspace_bytes(N, H, V):
@@ -378,7 +385,7 @@ def mop_vocab_loss_bwd(device, X, W_voc, targets, lse, dloss, dX, dW_voc, worksp
         workspace = _workspace(mop_vocab_bwd_workspace_bytes(N, H, V), X.device, stream)
     _check("mop_vocab_loss_bwd",
            lib().mop_vocab_loss_bwd(device, N, H, V, _ptr(X), _ptr(W_voc), _ptr(targets), _ptr(lse), _ptr(dloss),
-                                    _ptr(dX), _ptr(dW_voc), _ptr(workspace), _stream(stream)))
+                                    _ptr(dX), _ptr(dW_voc), _ptr(workspace), _stream(stream, device)))
     return workspace
 
 
@@ -395,7 +402,7 @@ def mop_vocab_distill_fwd(device, X, W_voc, teacher_idx, teacher_logits, tempera
     _check("mop_vocab_distill_fwd",
            lib().mop_vocab_distill_fwd(device, N, H, V, K, _ptr(X), _ptr(W_voc), _ptr(teacher_idx), _ptr(teacher_logits),
                                        _ptr(teacher_lse), temperature, _ptr(loss), _ptr(student), _ptr(lse), _ptr(workspace),
-                                       _stream(stream)))
+                                       _stream(stream, device)))
     return workspace
 
 
@@ -412,7 +419,7 @@ def mop_vocab_distill_bwd(device, X, W_voc, teacher_idx, teacher_logits, tempera
     _check("mop_vocab_distill_bwd",
            lib().mop_vocab_distill_bwd(device, N, H, V, K, _ptr(X), _ptr(W_voc), _ptr(teacher_idx), _ptr(teacher_logits),
                                        _ptr(teacher_lse), temperature, _ptr(student), _ptr(lse), _ptr(dloss), _ptr(dX),
-                                       _ptr(dW_voc), _ptr(workspace), _stream(stream)))
+                                       _ptr(dW_voc), _ptr(workspace), _stream(stream, device)))
     return workspace
 
 
@@ -425,7 +432,7 @@ def mop_profile_read(ctx, stream=None, max_names=64):
     names = (ctypes.c_char_p * max_names)()
     ms = (ctypes.c_float * max_names)()
     calls = (ctypes.c_int32 * max_names)()
-    n = lib().mop_profile_read(ctx.handle, _stream(stream), max_names, names, ms, calls)
+    n = lib().mop_profile_read(ctx.handle, _stream(stream, ctx.device), max_names, names, ms, calls)
     if n < 0:
         raise RuntimeError("mop_profile_read failed")
     return {names[i].decode(): (float(ms[i]), int(calls[i])) for i in range(n)}
