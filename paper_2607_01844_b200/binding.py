@@ -134,6 +134,26 @@ def _workspace(size, device, stream):
         return torch.empty(max(256, size), dtype=torch.uint8, device=device)
 
 
+def _tensors(call, device, names, tensors, least):
+    """Addresses of a call's tensors (None stays None), each with the bytes that the call uses of it.  The library sees addresses only, so
+    a tensor that is too short or on another device is refused here.  (The smallest calls take as long as their host side.)"""
+    try:
+        return [None if t is None else t.data_ptr() if t.nbytes >= need and t.get_device() == device and t.is_contiguous()
+                else _unlike(call, device, names, tensors, t, need) for t, need in zip(tensors, least)]
+    except AttributeError:                 # an address in a tensor's place
+        return [_unlike(call, device, names, tensors, t, need) for t, need in zip(tensors, least)]
+
+
+def _unlike(call, device, names, tensors, t, need):
+    at = _ptr(t)
+    if t is None or isinstance(t, int) or (t.nbytes >= need and t.get_device() == device):
+        return at
+    name = names.split()[next(i for i, other in enumerate(tensors) if other is t)]
+    if at % (256 if name == "workspace" else 16) == 0:        # (the library refuses the others)
+        raise MopError(f"{call}: {name} has {t.nbytes} bytes on {t.device}, {need} on device {device} are used", 1)
+    return at
+
+
 def _check(call, rc):
     if rc != MOP_OK:
         raise MopError(call, rc)
@@ -148,6 +168,7 @@ class Context:
                               int(host_io), route_path)
         self.handle = _P()
         self.device = device
+        self._balance = {}
         _check("mop_create", lib().mop_create(ctypes.byref(self.handle), ctypes.byref(self.shape), device))
 
     def close(self):
@@ -160,6 +181,18 @@ class Context:
             self.close()
         except Exception:
             pass
+
+    def balance_bytes(self, n_seq):
+        """Bytes that the balance loss's forward and backward use of each tensor, worked out once for a number of sequences."""
+        if n_seq not in self._balance:
+            T, d, E, k = self.shape.T, self.shape.d, self.shape.E, self.shape.k
+            size = {"logits": T * E * 4, "bias": E * 4, "topk_idx": T * k * 4, "seq_offsets": n_seq * 4 + 4, "counts": n_seq * E * 4,
+                    "prob": n_seq * E * 4, "loss": n_seq * 4, "dloss": n_seq * 4, "x": T * d * 2, "W_r": d * E * 4, "dlogits": T * E * 4,
+                    "dW_r": d * E * 4, "dbias": E * 4, "dX": T * d * 2}
+            self._balance[n_seq] = tuple(
+                tuple(mop_moe_balance_workspace_bytes(self, n_seq, backward) if n == "workspace" else size[n] for n in names.split())
+                for backward, names in enumerate((_BALANCE_FWD, _BALANCE_BWD)))
+        return self._balance[n_seq]
 
     @property
     def workspace_bytes(self):
@@ -262,20 +295,26 @@ def mop_moe_balance_workspace_bytes(ctx, n_seq, with_backward=False):
     return lib().mop_moe_balance_workspace_bytes(ctypes.byref(ctx.shape), n_seq, int(with_backward))
 
 
+_BALANCE_FWD = "logits bias topk_idx seq_offsets counts prob loss workspace"
+_BALANCE_BWD = "logits bias seq_offsets counts dloss x W_r dlogits dW_r dbias dX workspace"
+
+
 def mop_moe_balance_loss_fwd(ctx, logits, bias, topk_idx, seq_offsets, counts, prob, loss, workspace, stream=None):
     """Per sequence of a packed batch: expert counts, mean scores and the load-balance loss."""
-    _check("mop_moe_balance_loss_fwd",
-           lib().mop_moe_balance_loss_fwd(ctx.handle, loss.shape[0], _ptr(logits), _ptr(bias), _ptr(topk_idx), _ptr(seq_offsets),
-                                          _ptr(counts), _ptr(prob), _ptr(loss), _ptr(workspace), _stream(stream, ctx.device)))
+    n_seq = loss.shape[0]
+    a = _tensors("mop_moe_balance_loss_fwd", ctx.device, _BALANCE_FWD,
+                 (logits, bias, topk_idx, seq_offsets, counts, prob, loss, workspace), (ctx._balance.get(n_seq) or ctx.balance_bytes(n_seq))[0])
+    _check("mop_moe_balance_loss_fwd", lib().mop_moe_balance_loss_fwd(ctx.handle, n_seq, *a, _stream(stream, ctx.device)))
 
 
 def mop_moe_balance_loss_bwd(ctx, logits, bias, seq_offsets, counts, dloss, x, W_r, dlogits, dW_r, dbias, dX, accumulate, workspace,
                              stream=None):
     """Gradients of sum_s dloss[s] loss[s]; outputs that are None are not computed."""
+    n_seq = dloss.shape[0]
+    a = _tensors("mop_moe_balance_loss_bwd", ctx.device, _BALANCE_BWD,
+                 (logits, bias, seq_offsets, counts, dloss, x, W_r, dlogits, dW_r, dbias, dX, workspace), (ctx._balance.get(n_seq) or ctx.balance_bytes(n_seq))[1])
     _check("mop_moe_balance_loss_bwd",
-           lib().mop_moe_balance_loss_bwd(ctx.handle, dloss.shape[0], _ptr(logits), _ptr(bias), _ptr(seq_offsets), _ptr(counts),
-                                          _ptr(dloss), _ptr(x), _ptr(W_r), int(accumulate), _ptr(dlogits), _ptr(dW_r), _ptr(dbias),
-                                          _ptr(dX), _ptr(workspace), _stream(stream, ctx.device)))
+           lib().mop_moe_balance_loss_bwd(ctx.handle, n_seq, *a[:7], int(accumulate), *a[7:], _stream(stream, ctx.device)))
 
 
 def mop_moe_chunked_workspace_bytes(ctx, n_chunks, with_backward=False):
@@ -397,12 +436,14 @@ def mop_vocab_distill_fwd(device, X, W_voc, teacher_idx, teacher_logits, tempera
                           workspace=None, stream=None):
     """loss[n] = KL divergence of the student from the teacher over the teacher's entries; student = logits at those entries."""
     (N, H), V, K = X.shape, W_voc.shape[1], teacher_idx.shape[1]
+    need = mop_vocab_distill_workspace_bytes(N, H, V, K)
     if workspace is None:
-        workspace = _workspace(mop_vocab_distill_workspace_bytes(N, H, V, K), X.device, stream)
+        workspace = _workspace(need, X.device, stream)
+    a = _tensors("mop_vocab_distill_fwd", device, "X W_voc teacher_idx teacher_logits teacher_lse loss student lse workspace",
+                 (X, W_voc, teacher_idx, teacher_logits, teacher_lse, loss, student, lse, workspace),
+                 (N * H * 2, H * V * 2, N * K * 4, N * K * 4, N * 4, N * 4, N * K * 4, N * 4, need))
     _check("mop_vocab_distill_fwd",
-           lib().mop_vocab_distill_fwd(device, N, H, V, K, _ptr(X), _ptr(W_voc), _ptr(teacher_idx), _ptr(teacher_logits),
-                                       _ptr(teacher_lse), temperature, _ptr(loss), _ptr(student), _ptr(lse), _ptr(workspace),
-                                       _stream(stream, device)))
+           lib().mop_vocab_distill_fwd(device, N, H, V, K, *a[:5], temperature, *a[5:], _stream(stream, device)))
     return workspace
 
 
@@ -414,12 +455,14 @@ def mop_vocab_distill_bwd(device, X, W_voc, teacher_idx, teacher_logits, tempera
                           teacher_lse=None, workspace=None, stream=None):
     """dX, dW_voc of sum_n dloss[n] loss[n]; student and lse are the forward's."""
     (N, H), V, K = X.shape, W_voc.shape[1], teacher_idx.shape[1]
+    need = mop_vocab_distill_bwd_workspace_bytes(N, H, V, K)
     if workspace is None:
-        workspace = _workspace(mop_vocab_distill_bwd_workspace_bytes(N, H, V, K), X.device, stream)
+        workspace = _workspace(need, X.device, stream)
+    a = _tensors("mop_vocab_distill_bwd", device, "X W_voc teacher_idx teacher_logits teacher_lse student lse dloss dX dW_voc workspace",
+                 (X, W_voc, teacher_idx, teacher_logits, teacher_lse, student, lse, dloss, dX, dW_voc, workspace),
+                 (N * H * 2, H * V * 2, N * K * 4, N * K * 4, N * 4, N * K * 4, N * 4, N * 4, N * H * 2, H * V * 2, need))
     _check("mop_vocab_distill_bwd",
-           lib().mop_vocab_distill_bwd(device, N, H, V, K, _ptr(X), _ptr(W_voc), _ptr(teacher_idx), _ptr(teacher_logits),
-                                       _ptr(teacher_lse), temperature, _ptr(student), _ptr(lse), _ptr(dloss), _ptr(dX),
-                                       _ptr(dW_voc), _ptr(workspace), _stream(stream, device)))
+           lib().mop_vocab_distill_bwd(device, N, H, V, K, *a[:5], temperature, *a[5:], _stream(stream, device)))
     return workspace
 
 
