@@ -396,9 +396,11 @@ mop_status mop_vocab_distill_fwd(int device, int32_t N, int32_t H, int32_t V, in
 /* Its gradients, with an upstream weight dloss[n] per token and Q[n] = sum_k q[n,k]:
  *   dY[n,v] = dloss[n] / temperature (Q[n] exp(s[n,v] - lse[n]) - sum of the q[n,k] with teacher_idx[n,k] = v),
  *   dX = dY W_voc^T,   dW_voc = X^T dY
- * in blocks of vocabulary columns, as mop_vocab_loss_bwd (as many as keep N x columns of dY at 2^28 elements, at least 8192).  student
- * and lse are the forward's.  dX [N,H] bf16 out, dW_voc [H,V] bf16 out (both overwritten).  dY is rounded to bf16 before its products;
- * with up to 128 tokens, where these roundings do not average out, to two bf16 pieces (16 bits).
+ * in blocks of vocabulary columns, as mop_vocab_loss_bwd: as many as keep N x columns of dY at 2^28 elements, but at least 8192.  student
+ * and lse are the forward's.  dX [N,H] bf16 out, dW_voc [H,V] bf16 out (both overwritten).  dY is rounded before its products: with up to
+ * 128 tokens to two bf16 pieces (16 bits, twice the memory), and the gradients are as exact as their own rounding; with more to one, as in
+ * mop_vocab_loss_bwd, and they are about 1.4 times as far off as that (1.1 to 1.9 where few tokens have a weight), single rows of dX up to
+ * about 3 times.
  * workspace: mop_vocab_distill_bwd_workspace_bytes bytes. */
 size_t mop_vocab_distill_bwd_workspace_bytes(int32_t N, int32_t H, int32_t V, int32_t K);
 mop_status mop_vocab_distill_bwd(int device, int32_t N, int32_t H, int32_t V, int32_t K, const void* X, const void* W_voc,

@@ -104,8 +104,8 @@ __device__ __forceinline__ void bal_scores(const BalShape& s, float (&z)[4 * NV]
 
 // ------------------------------------------------------------------------------------------ forward
 // Bound by latency: T 16384, E 256 takes 12 us for 17.8 MB (a launch, the search for the block's sequence, three or four rounds of one
-// row per warp, 16 warps' sums through shared memory), T 256, E 8 in one block 5.8.  In a training loop the calls themselves, 16 us,
-// take longer than either.
+// row per warp, 16 warps' sums through shared memory), T 256, E 8 in one block 5.8.  In a training loop the calls themselves take
+// 16 us with one launch and 19 with two, about what the two kernels of the former, one after the other, take as well (12 + 7.6).
 // Sequences are cut where blocks of `chunk` tokens end.  A block finishes the sequences that lie inside its chunk; of one that goes
 // on beyond it, it leaves the sums: slot 0 where the sequence began before the chunk, slot 1 where it begins in it.
 struct BalFwdArgs {

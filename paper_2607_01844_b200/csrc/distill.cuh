@@ -15,15 +15,20 @@
 // a pair would multiply as much again in vain, and half of its stages would hold X: reading W is all there is then, and the product
 // runs on single CTAs, tiles of 128 rows and up to 256 columns, whose rings hold as many bytes of W in flight as shared memory takes.
 //
-// One bf16 dY has an error of up to 2^-8 in each of its elements.  In the gradients these average out over the tokens, to about what the
-// rounding of the gradients themselves costs, but with few tokens they are the error of one or two elements that outweigh the rest
-// (temperature 1, H 512, V 16384, K 5 to 126, error of dX over that of rounding it once: 1.4 in the middle, up to 1.9 with 2 tokens, 1.6
-// with 16, 1.5 with 64 to 128, 1.49 with 192; 1.00 with two pieces).  There the products wait for W, and a second piece with what the first
-// leaves out costs less than its operations (backward in us, one piece and two: N 10, H 1936, V 28800 86, 90; N 16, H 4096, V 64000 300,
-// 305; N 64, H 2048, V 32000 100, 108; N 100, H 2048, V 50304 150, 170; N 128, H 7168, V 131072 1028, 1249).
+// One bf16 dY has an error of up to 2^-8 in each of its elements.  A row of dX is a sum over the vocabulary of its own token's dY, dW one
+// over the tokens, and either way the errors add up as the terms do: they never average out, and with one piece the gradients are further
+// off than their own rounding whatever the number of tokens.  Error over that of rounding them once, H 256, V 4096, K 5 and 64: dX as
+// a whole 1.35 to 1.5 with 129, 300 and 2000 tokens alike, its worst row 2.3 to 2.7 (where one or two elements of dY outweigh the
+// rest), dW 1.35 to 1.45; 1.1 to 1.9 where three tokens alone have a weight.  A second piece with what the first leaves out makes it 1.00,
+// and doubles the two products behind it.  Up to 128 tokens these wait for W, and it costs 2 to 21 % (backward in us, one piece and two:
+// N 10, H 1936, V 28800 86, 90; N 16, H 4096, V 64000 300, 305; N 64, H 2048, V 32000 100, 108; N 100, H 2048, V 50304 150, 170; N 128,
+// H 7168, V 131072 1028, 1249).  Above, the tensor cores are the limit, and it would be more than half of the call again (N 1537,
+// H 2048, V 50304: the two products are 249 and 220 of 870 us): one piece, as in mop_vocab_loss_bwd.
+// Besides, VD_P sums its logits over all of H at once, where the tensor core truncates: 8e-6 of their size at H 7168, 2e-6 at 2048 (N 64; error of
+// p 1.4e-5 with logits of 1.7, 6.9e-5 with logits of 8.5).  In dX that is nothing at the former and 1 % of its rounding at the latter.
 //
 // What bounds them, measured: many rows the tensor cores (VD_L N 2048, H 2048, V 32000 177 us, 1.52 PFLOP/s, where cuBLAS takes 180 for
-// the same product with its bf16 store; N 8192, H 7168, V 131072 11.8 to 13.4 ms under the power cap, cuBLAS 11.1); few rows DRAM (VD_L
+// the same product with its bf16 store; N 8192, H 7168, V 131072 11.8 to 14.1 ms under the power cap, cuBLAS 11.1); few rows DRAM (VD_L
 // N 64, H 2048, V 32000 27 us for 131 MB, 4.8 TB/s, against 30 us for a plain read of as many bytes; VD_W N 256 36 us for 131 MB of
 // stores against 38 for a plain fill; VD_R T 16384, d 7168, E 256 69 us for 235 MB against 66).  Stores alone run at 3.6 to 3.9 TB/s on this part,
 // so neither a deeper ring, nor more store boxes, nor evict-first lines, nor another tile order made VD_W or VD_R faster.
@@ -1004,7 +1009,8 @@ inline bool vd_map_out(const TcPlan* p, CUtensorMap* m, const void* base, uint64
     return tc_map_2d_pitch(p, m, base, rows, cols, pitch, 128);
 }
 
-// Vocabulary columns whose logit gradients are live at a time: as many as keep dY at 2^28 elements (512 MiB), at least 8192, in blocks
+// Vocabulary columns whose logit gradients are live at a time: as many as keep a piece of dY at 2^28 elements (512 MiB; 1 GiB for the two pieces
+// of up to 128 tokens), but at least 8192, which is more than that with more than 32768 tokens; in blocks
 // of about equal width.  Wide blocks mean few launches, long sums and few passes over the fp32 sums of dX.  Backward in us, blocks of up to
 // 8192, 16384, 32768, 65536 columns and all: N 1537, H 2048, V 50304 930, 829, 770, 722, 723; N 4096, H 7168, V 131072 18150, 17900,
 // 17500, 17350, 18500; N 8192 36300, 36550, 37200, 37200, 39500; N 256, H 2048, V 32000 243 in four and 123 in one.
