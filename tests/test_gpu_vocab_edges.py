@@ -60,3 +60,54 @@ def test_a_default_workspace_belongs_to_the_stream_of_the_call(raw):
         with torch.cuda.stream(side):
             assert torch.empty((size,), dtype=torch.uint8, device="cuda").data_ptr() == at
     side.synchronize()
+
+
+def test_calls_that_overlap_on_two_streams():
+    """Two sequences of the losses' calls at once, each with a context, workspaces and outputs of its own: the same bits as one after the
+    other.  Replayed graphs that share their workspaces, one behind the other on a stream, give them too."""
+    from test_gpu_balance import SIGMOID, Case
+    from test_gpu_balance import PRE
+
+    def job(i):
+        c = Case(1500 + 64 * i, 264, 40, 4, SIGMOID, PRE, [5, 700, 1400], seed=i)
+        g = torch.Generator(device="cuda").manual_seed(i)
+        N, H, V, K = (100, 300)[i], 264, 8192 + 520, 20
+        X = torch.randn((N, H), generator=g, device="cuda").to(torch.bfloat16)
+        W = (torch.randn((H, V), generator=g, device="cuda") * 0.1).to(torch.bfloat16)
+        ids = torch.randint(0, V, (N, K), generator=g, device="cuda", dtype=torch.int32)
+        t, dloss = torch.randn((N, K), generator=g, device="cuda"), torch.randn((N,), generator=g, device="cuda")
+        wf, wb = c.workspace(False), c.workspace(True)
+        df = torch.empty(binding.mop_vocab_distill_workspace_bytes(N, H, V, K), dtype=torch.uint8, device="cuda")
+        db = torch.empty(binding.mop_vocab_distill_bwd_workspace_bytes(N, H, V, K), dtype=torch.uint8, device="cuda")
+
+        def run():
+            fwd = c.forward(ws=wf)
+            out = c.backward(fwd[0], c.outputs(0.5), True, ws=wb)
+            loss, lse, student = torch.empty((N,), device="cuda"), torch.empty((N,), device="cuda"), torch.empty((N, K), device="cuda")
+            dX, dW = torch.empty_like(X), torch.empty_like(W)
+            binding.mop_vocab_distill_fwd(0, X, W, ids, t, 1.0, loss, student, lse, None, df)
+            binding.mop_vocab_distill_bwd(0, X, W, ids, t, 1.0, student, lse, dloss, dX, dW, None, db)
+            return [*fwd, *out.values(), loss, lse, student, dX, dW]
+        return run
+    jobs = [job(0), job(1)]
+    want = [run() for run in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(10):
+        got = []
+        for run, stream in zip(jobs, streams):
+            with torch.cuda.stream(stream):
+                got.append(run())
+        torch.cuda.synchronize()
+        for a, b in zip(want, got):
+            assert all(torch.equal(x.nan_to_num(), y.nan_to_num()) for x, y in zip(a, b))
+    graphs = []
+    for run in (jobs[0], jobs[0]):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            graphs.append((graph, run()))
+    for graph, out in graphs * 3:
+        graph.replay()
+    torch.cuda.synchronize()
+    for _, out in graphs:
+        assert all(torch.equal(x.nan_to_num(), y.nan_to_num()) for x, y in zip(want[0], out))
